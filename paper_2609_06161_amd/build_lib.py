@@ -1,5 +1,6 @@
-"""Build ``libaf1.so`` (HIP kernels + C ABI) and ``libaf1_nabf.so`` (the NABF
-building blocks) for gfx950 with hipcc.
+"""Build ``libaf1.so`` (HIP kernels + C ABI), ``libaf1_nabf.so`` (the NABF
+building blocks) and ``libaf1_head.so`` (the output head and its losses) for
+gfx950 with hipcc.
 
 Every call recompiles.  Objects go to ``_build/`` beside this file; the
 shared library lands in the package directory, where the binding loads it.
@@ -15,6 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libaf1.so")
 NABF_LIB = os.path.join(HERE, "libaf1_nabf.so")
+HEAD_LIB = os.path.join(HERE, "libaf1_head.so")
+HEAD_SRCS = ("af1_head_api.hip", "af1_fp8.hip", "af1_logits.hip")
 # libaf1.so with -DAF1_TEST_BUILD: tests only, nothing else loads it
 TEST_LIB = os.path.join(HERE, "libaf1_test.so")
 TEST_SRCS = ("af1_gemv.hip", "af1_gemm.hip")  # the sources that it compiles differently
@@ -55,9 +58,9 @@ def _link(out: str, objs, libs, verbose: bool) -> None:
 
 def build(verbose: bool = False) -> str:
     """Compile every source; link libaf1.so (the layer), its test build
-    libaf1_test.so, and libaf1_nabf.so (the offline NABF building blocks, which
-    also need rocBLAS and rocSOLVER and reuse the sign-packing kernel).  Returns
-    the path of libaf1.so."""
+    libaf1_test.so, libaf1_nabf.so (the offline NABF building blocks, which
+    also need rocBLAS and rocSOLVER and reuse the sign-packing kernel) and
+    libaf1_head.so (the output head).  Returns the path of libaf1.so."""
     os.makedirs(BUILD, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
     with cf.ThreadPoolExecutor(max_workers=8) as ex:
@@ -66,9 +69,11 @@ def build(verbose: bool = False) -> str:
         objs = dict(zip(srcs, ex.map(lambda s: _compile(s, verbose), srcs)))
     nabf_src = os.path.join(CSRC, "af1_nabf.hip")
     pack_src = os.path.join(CSRC, "af1_pack.hip")
-    _link(LIB, [o for s, o in objs.items() if s != nabf_src], [], verbose)
-    _link(TEST_LIB, [tests[s].result() if s in tests else o for s, o in objs.items()
-                     if s != nabf_src], [], verbose)
+    head_srcs = [os.path.join(CSRC, s) for s in HEAD_SRCS]
+    layer = [s for s in objs if s != nabf_src and s not in head_srcs]
+    _link(LIB, [objs[s] for s in layer], [], verbose)
+    _link(TEST_LIB, [tests[s].result() if s in tests else objs[s] for s in layer], [], verbose)
+    _link(HEAD_LIB, [objs[s] for s in head_srcs], [], verbose)
     _link(NABF_LIB, [objs[nabf_src], objs[pack_src]],
           ["-L/opt/rocm/lib", "-lrocsolver", "-lrocblas"], verbose)
     return LIB

@@ -1,0 +1,298 @@
+"""The output head on torch tensors: the 8-bit block-scaled linear, the log
+probabilities of given tokens and the KL divergence to a teacher, as plain
+calls that check their tensors, provide outputs and workspaces where none are
+given, and forward to the C entry points (include/af1_head.h).
+
+Every call runs on the device of its tensors, on `stream` or that device's
+current stream.  bfloat16 tensors may also be given as int16 bit patterns, the
+form in which DeviceLayer returns its outputs.  Workspaces (`ws`) are optional;
+one that is passed in must not be used by another call at the same time, which
+two captured graphs that share it would do if they were replayed together.
+"""
+import contextlib
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import af1, head
+from .layer import on_stream
+
+FORMATS = {"e4m3": head.AF1_FP8_E4M3, "e5m2": head.AF1_FP8_E5M2}
+DENSE = {torch.float32: af1.AF1_SRC_F32, torch.bfloat16: af1.AF1_SRC_BF16,
+         torch.float16: af1.AF1_SRC_F16, torch.int16: af1.AF1_SRC_BF16}
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _dense(t, name):
+    _need(isinstance(t, torch.Tensor) and t.is_cuda, f"{name} must be a GPU tensor")
+    _need(t.dtype in DENSE, f"{name} must be float32, bfloat16, float16 or int16 (bfloat16 "
+                            f"patterns), not {t.dtype}")
+    return DENSE[t.dtype]
+
+
+def _array(t, name, device, dtype, shape):
+    """Checks an optional contiguous array of a call."""
+    if t is None:
+        return
+    _need(isinstance(t, torch.Tensor) and t.device == device, f"{name} must be on {device}")
+    _need(t.dtype == dtype, f"{name} must be {dtype}, not {t.dtype}")
+    _need(tuple(t.shape) == tuple(shape) and t.is_contiguous(),
+          f"{name} must be contiguous of shape {tuple(shape)}, not {tuple(t.shape)}")
+
+
+def _workspace(ws, need, device):
+    if ws is None:
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _need(ws.device == device and ws.is_contiguous(), f"ws must be contiguous on {device}")
+    return ws
+
+
+def _bytes(ws):
+    return 0 if ws is None else ws.numel() * ws.element_size()
+
+
+@contextlib.contextmanager
+def _on(device, stream):
+    """The device of the tensors and the stream that the kernels run on."""
+    with torch.cuda.device(device), on_stream(stream):
+        yield
+
+
+class Fp8Matrix:
+    """A rows x cols matrix in 8-bit floating point ("e4m3" or "e5m2") with a
+    power-of-two scale for each block of 128 x 128: codes and scales as uint8
+    tensors in the storage of af1_fp8_matrix."""
+
+    def __init__(self, rows, cols, fmt, codes, scales):
+        _need(fmt in FORMATS, f"fmt must be one of {tuple(FORMATS)}, not {fmt!r}")
+        self.rows, self.cols, self.fmt = int(rows), int(cols), fmt
+        _need(head.af1_fp8_code_bytes(self.rows, self.cols) > 0,
+              f"rows and cols must be in 1..{af1.AF1_MAX_DIM}, not {rows} x {cols}")
+        for t, need, name in ((codes, head.af1_fp8_code_bytes(self.rows, self.cols), "codes"),
+                              (scales, head.af1_fp8_scale_bytes(self.rows, self.cols), "scales")):
+            _need(isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.uint8
+                  and t.is_contiguous() and t.numel() == need,
+                  f"{name} must be a contiguous GPU tensor of {need} uint8")
+        _need(codes.device == scales.device, "codes and scales must be on one device")
+        self.codes, self.scales = codes, scales
+        self.desc = head.make_matrix(self.rows, self.cols, FORMATS[fmt], codes, scales)
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    @classmethod
+    def empty(cls, rows, cols, fmt="e4m3", device="cuda"):
+        code, scale = head.af1_fp8_code_bytes(rows, cols), head.af1_fp8_scale_bytes(rows, cols)
+        return cls(rows, cols, fmt, torch.empty(code, dtype=torch.uint8, device=device),
+                   torch.empty(scale, dtype=torch.uint8, device=device))
+
+    @classmethod
+    def quantize(cls, src, fmt="e4m3", out=None, stream=None):
+        """The 8-bit form of a dense contiguous matrix."""
+        dtype = _dense(src, "src")
+        _need(src.dim() == 2 and src.is_contiguous(), "src must be a contiguous matrix")
+        rows, cols = src.shape
+        with _on(src.device, stream):
+            if out is None:
+                out = cls.empty(rows, cols, fmt, src.device)
+            _need((out.rows, out.cols, out.fmt) == (rows, cols, fmt) and out.device == src.device,
+                  f"out must be a {rows} x {cols} {fmt} matrix on {src.device}")
+            head.af1_fp8_quantize(src, dtype, rows, cols, FORMATS[fmt], out.codes, out.scales,
+                                  stream)
+        return out
+
+    def dequantize(self, dtype=torch.bfloat16, out=None, stream=None):
+        """The values that the matrix stands for."""
+        _need(dtype in DENSE, f"dtype must be one of {tuple(DENSE)}, not {dtype}")
+        with _on(self.device, stream):
+            if out is None:
+                out = torch.empty((self.rows, self.cols), dtype=dtype, device=self.device)
+            _array(out, "out", self.device, dtype, (self.rows, self.cols))
+            head.af1_fp8_dequantize(self.desc, out, DENSE[dtype], stream)
+        return out
+
+    def transpose(self, stream=None):
+        """The transposed matrix; codes and scales are moved, nothing rounds."""
+        with _on(self.device, stream):
+            out = Fp8Matrix.empty(self.cols, self.rows, self.fmt, self.device)
+            head.af1_fp8_transpose(self.desc, out.codes, out.scales, stream)
+        return out
+
+
+class Fp8Linear:
+    """y = x W^T with W an Fp8Matrix of m = rows by n = cols.  Activations are
+    rounded to 8 bits inside the call, each token's 128 columns at a scale of
+    their own; sums are fp32."""
+
+    def __init__(self, weight, transposed=None):
+        self.weight = weight
+        self.m, self.n = weight.rows, weight.cols
+        if transposed is not None:
+            _need((transposed.rows, transposed.cols) == (self.n, self.m),
+                  f"transposed must be {self.n} x {self.m}")
+        self._T = transposed
+
+    @classmethod
+    def from_dense(cls, w, fmt="e4m3", stream=None):
+        return cls(Fp8Matrix.quantize(w, fmt, stream=stream))
+
+    def transposed(self, stream=None):
+        """The weight transposed, made once (the weight is frozen)."""
+        if self._T is None:
+            self._T = self.weight.transpose(stream)
+        return self._T
+
+    def workspace(self, T, grad=False):
+        """A workspace for calls of up to T tokens."""
+        m, n = (self.n, self.m) if grad else (self.m, self.n)
+        need = head.af1_fp8_linear_workspace_bytes(m, n, T)
+        _need(need > 0 or 0 <= T <= head.AF1_HEAD_MAX_TOKENS, f"T must be at most "
+              f"{head.AF1_HEAD_MAX_TOKENS}")
+        return torch.empty(max(need, 16), dtype=torch.uint8, device=self.weight.device)
+
+    def forward(self, x, y=None, ws=None, fmt="e4m3", dtype=torch.bfloat16, stream=None):
+        """[T, n] -> [T, m] of y's type, or of `dtype` (float32, bfloat16)."""
+        return _linear(self.weight, x, y, ws, fmt, dtype, stream)
+
+    def input_grad(self, dy, dx=None, ws=None, fmt="e5m2", dtype=torch.bfloat16, stream=None):
+        """dx = dy W, [T, m] -> [T, n]."""
+        with _on(self.weight.device, stream):
+            WT = self.transposed(stream)
+        return _linear(WT, dy, dx, ws, fmt, dtype, stream)
+
+
+def _linear(W, x, y, ws, fmt, dtype, stream):
+    x_dtype = _dense(x, "x")
+    _need(fmt in FORMATS, f"fmt must be one of {tuple(FORMATS)}, not {fmt!r}")
+    _need(x.dim() == 2 and x.shape[1] == W.cols and x.is_contiguous() and x.device == W.device,
+          f"x must be contiguous of shape [T, {W.cols}] on {W.device}")
+    T = x.shape[0]
+    with _on(W.device, stream):
+        if y is None:
+            y = torch.empty((T, W.rows), dtype=dtype, device=x.device)
+        y_dtype = _dense(y, "y")
+        _array(y, "y", x.device, y.dtype, (T, W.rows))
+        ws = _workspace(ws, head.af1_fp8_linear_workspace_bytes(W.rows, W.cols, T), x.device)
+        head.af1_fp8_linear(W.desc, x, x_dtype, FORMATS[fmt], T, y, y_dtype, ws, _bytes(ws),
+                            stream)
+    return y
+
+
+def _logits(t, name):
+    """(dtype code, T, V, row stride) of a [T, V] tensor whose rows may be apart."""
+    dtype = _dense(t, name)
+    _need(t.dim() == 2 and t.shape[1] >= 1, f"{name} must be [T, V]")
+    T, V = t.shape
+    _need(V == 1 or t.stride(1) == 1, f"{name}'s rows must be contiguous")
+    ld = t.stride(0) if T > 1 else V
+    _need(ld >= V, f"{name}'s rows must not overlap")
+    return dtype, T, V, ld
+
+
+class TokenLogprobs(NamedTuple):
+    """What token_logprobs gives: fp32[T] each, the alternatives [T, k], and
+    `saved` for its backward."""
+    logprob: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_logprob: Optional[torch.Tensor]
+    top_index: Optional[torch.Tensor]
+    saved: torch.Tensor
+
+
+def token_logprobs(logits, targets=None, k=0, scale=1.0, ws=None, stream=None):
+    """Log probabilities of the given tokens under softmax(scale * logits), the
+    entropy, and the k most likely tokens (af1_token_logprobs)."""
+    dtype, T, V, ld = _logits(logits, "logits")
+    dev = logits.device
+    _array(targets, "targets", dev, torch.int64, (T,))
+    _need(0 <= k <= head.AF1_HEAD_MAX_TOP, f"k must be in 0..{head.AF1_HEAD_MAX_TOP}, not {k}")
+    with _on(dev, stream):
+        # one block: entropy, lse, logprob and alternatives behind the saved rows
+        buf = torch.empty((7 + k) * T, dtype=torch.float32, device=dev)
+        saved, entropy, lse = buf[:4 * T].view(T, 4), buf[4 * T:5 * T], buf[5 * T:6 * T]
+        logprob = buf[6 * T:7 * T] if targets is not None else None
+        top = buf[7 * T:].view(T, k) if k else None
+        index = torch.empty((T, k), dtype=torch.int64, device=dev) if k else None
+        ws = _workspace(ws, head.af1_token_logprobs_workspace_bytes(T, V, k), dev)
+        head.af1_token_logprobs(logits, dtype, T, V, ld, scale, targets, logprob, entropy, lse, k,
+                                top, index, saved, ws, _bytes(ws), stream)
+    return TokenLogprobs(logprob, entropy, lse, top, index, saved)
+
+
+def token_logprobs_backward(logits, targets, result, g_logprob=None, g_entropy=None, scale=1.0,
+                            dlogits=None, stream=None):
+    """The logits' gradient for the gradients of token_logprobs' logprob and
+    entropy (either may be None); `result` is what it returned.  dlogits may be
+    the logits themselves."""
+    dtype, T, V, ld = _logits(logits, "logits")
+    dev = logits.device
+    _array(targets, "targets", dev, torch.int64, (T,))
+    _array(g_logprob, "g_logprob", dev, torch.float32, (T,))
+    _array(g_entropy, "g_entropy", dev, torch.float32, (T,))
+    _array(result.saved, "result.saved", dev, torch.float32, (T, 4))
+    _need(g_logprob is None or targets is not None, "g_logprob needs targets")
+    with _on(dev, stream):
+        dlogits, ldd = _gradient(dlogits, logits)
+        head.af1_token_logprobs_backward(logits, dtype, T, V, ld, scale, targets, result.saved,
+                                         g_logprob, g_entropy, dlogits, ldd, stream)
+    return dlogits
+
+
+def _gradient(out, logits):
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    _need(out.dtype == logits.dtype and out.shape == logits.shape
+          and out.device == logits.device, "the gradient must match the logits")
+    return out, _logits(out, "the gradient")[3]
+
+
+def distill_kl(student, teacher, scale=1.0, weight=None, grad=True, dstudent=None, ws=None,
+               stream=None):
+    """(kl, dstudent): each token's KL divergence from softmax(scale * teacher)
+    to softmax(scale * student), and the student logits' gradient of
+    sum_t weight[t] kl[t] (weight None: ones; grad False: None).  dstudent may
+    be the student itself."""
+    dtype, T, V, ld_s = _logits(student, "student")
+    t_dtype, _, _, ld_t = _logits(teacher, "teacher")
+    dev = student.device
+    _need(teacher.shape == student.shape and t_dtype == dtype and teacher.device == dev,
+          "student and teacher must have one shape, type and device")
+    _array(weight, "weight", dev, torch.float32, (T,))
+    with _on(dev, stream):
+        kl = torch.empty(T, dtype=torch.float32, device=dev)
+        ldd = 0
+        if grad or dstudent is not None:
+            dstudent, ldd = _gradient(dstudent, student)
+        ws = _workspace(ws, head.af1_distill_kl_workspace_bytes(T, V), dev)
+        head.af1_distill_kl(student, teacher, dtype, T, V, ld_s, ld_t, scale, weight, kl, dstudent,
+                            ldd, ws, _bytes(ws), stream)
+    return kl, dstudent
+
+
+def reconstruction_step(layer, output, x, teacher, weight=None, scale=1.0, grads=None,
+                        accumulate=False, want_dx=True, stream=None):
+    """One step of the scale-only reconstruction (Sec. 4.1, label
+    eq:scale_only_kl) for a factorized linear below an 8-bit output head: the
+    student logits head(layer(x)), their KL divergence to the teacher's, and
+    the gradients of the layer's three scale vectors and of x.
+
+    layer: DeviceLayer; output: Fp8Linear with n = layer.m; x: [T, layer.n]
+    bfloat16; teacher: [T, V] logits (float32 or bfloat16).  Returns (kl [T],
+    dx or None, (ds_out, ds_mid, ds_in)); the sum of weight * kl is the loss."""
+    _need(output.n == layer.m, f"the head reads {output.n} features, the layer gives {layer.m}")
+    _need(teacher.dtype in (torch.float32, torch.bfloat16), "teacher must be float32 or bfloat16")
+    xb = x.view(torch.int16) if x.dtype == torch.bfloat16 else x
+    hidden, saved = layer.forward_train(xb, stream=stream)
+    logits = output.forward(hidden, dtype=teacher.dtype, stream=stream)
+    # the gradient takes the logits' place
+    kl, dlogits = distill_kl(logits, teacher, scale, weight, dstudent=logits, stream=stream)
+    dh = output.input_grad(dlogits, stream=stream)
+    dx, grads = layer.backward(xb, dh.view(torch.int16), saved, grads=grads,
+                               accumulate=accumulate, stream=stream, want_dx=want_dx)
+    return kl, dx, grads
