@@ -20,6 +20,7 @@ using af1::f16_to_f32;
 using af1::f32_to_bf16;
 using af1::f32_to_f16;
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
@@ -225,61 +226,269 @@ __device__ __forceinline__ void to_bf16(const int *w, bf8v (&out)[2]) {
   }
 }
 
-// tmp += products of 64 columns, exact and unscaled.
-template <int kWFormat, int kXFormat>
-__device__ __forceinline__ v16f mul_bf16(v8i w, v8i x, v16f tmp) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int wi[4] = {w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]};
-    const int xi[4] = {x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
-    bf8v a[2], b[2];
-    to_bf16<kWFormat>(wi, a);
-    to_bf16<kXFormat>(xi, b);
-    tmp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[0], tmp, 0, 0, 0);
-    tmp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1], b[1], tmp, 0, 0, 0);
-  }
-  return tmp;
+// acc += products of 64 columns at the scales (E8M0): W's is byte 0 of sw, the
+// tokens' byte kByte of sx.
+template <int kWFormat, int kXFormat, int kByte>
+__device__ __forceinline__ v16f mfma_scaled(v8i w, v8i x, v16f acc, int sw, int sx) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, acc, kWFormat, kXFormat, 0, sw,
+                                                         kByte, sx);
 }
 
-// A wave computes 32 rows of the weight x 32 tokens, operands straight from
-// memory.  Token tiles hold 128 rows, so the operand reads stay inside them.
-template <int kXFormat, int kWFormat, int kOut>
-__global__ __launch_bounds__(256) void linear_kernel(const uint8_t *wcodes, const uint8_t *wscales,
-                                                     XTiles x, int64_t T, int64_t m, int64_t n,
-                                                     void *y) {
-  const int64_t C = (n + kBlk - 1) / kBlk;
-  const int64_t strips = (m + 31) / 32;
-  const int64_t strip = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (strip >= strips) return;
-  const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
-  const int64_t t0 = (int64_t)blockIdx.y * 32, i0 = strip * 32;
-  const uint8_t *xa = x.codes + t0 / kBlk * C * kTileBytes + (t0 % kBlk + r) * kBlk + h * 32;
-  const uint8_t *xs = x.scales + t0 / kBlk * C * kBlk + r * 4 + t0 % kBlk / 32;
-  const uint8_t *wb = wcodes + i0 / kBlk * C * kTileBytes + (i0 % kBlk + r) * kBlk + h * 32;
-  const uint8_t *wsc = wscales + i0 / kBlk * C;
-  v16f acc = {};
-  for (int64_t J = 0; J < C; ++J) {
-    const int sx = xs[J * kBlk], sw = wsc[J];
-    v16f tmp = {};
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const v8i a = *reinterpret_cast<const v8i *>(wb + J * kTileBytes + s * 64);
-      const v8i b = *reinterpret_cast<const v8i *>(xa + J * kTileBytes + s * 64);
-      if constexpr (kOut == AF1_SRC_BF16)
-        acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, kWFormat, kXFormat, 0, sw,
-                                                              0, sx);
-      else
-        tmp = mul_bf16<kWFormat, kXFormat>(a, b, tmp);
-    }
-    if constexpr (kOut != AF1_SRC_BF16)
-#pragma unroll
-      for (int g = 0; g < 16; ++g) acc[g] += ldexpf(tmp[g], sx + sw - 254);
+// Four floats and eight bfloat16 that need their element's alignment only.
+struct __attribute__((packed, aligned(4))) Four {
+  float v[4];
+};
+struct __attribute__((packed, aligned(2))) Chunk {
+  uint32_t v[4];
+};
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  return (uint32_t)f32_to_bf16(a) | (uint32_t)f32_to_bf16(b) << 16;
+}
+
+// The first `left` (or all) of eight values.
+__device__ __forceinline__ void store8_bf16(uint16_t *p, int64_t left, uint4 v) {
+  if (left >= 8) {
+    *reinterpret_cast<Chunk *>(p) = Chunk{{v.x, v.y, v.z, v.w}};
+    return;
   }
-  const int64_t t = t0 + r;
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int g = 0; g < 16; ++g) {
-    const int64_t i = i0 + (g & 3) + 8 * (g >> 2) + 4 * h;
-    if (t < T && i < m) store_dense<kOut>(y, t * m + i, acc[g]);
+  for (int e = 0; e < 8; ++e)
+    if (e < left) p[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+}
+
+// ---------------------------------------------------------------------------
+// Tiled product.  A workgroup of kWR x kWC waves computes kTW rows of W x kTX
+// tokens; a wave kFR x kFC pieces of 32 x 32.  A step is one column block: the
+// tile rows' 128 bytes go from memory straight into LDS (buffer loads with an
+// LDS destination), double-buffered: a step waits for its own copies, meets
+// the other waves once, issues the next step's copies and multiplies.
+//
+// LDS holds rows of 128 bytes, eight chunks of 16.  A copy instruction writes
+// 64 consecutive chunks (eight rows), one a lane, and a lane chooses its
+// source: chunk c of row r is kept at position c XOR (r mod 8), so that the
+// operand reads of eight consecutive rows fall in distinct banks.
+// ---------------------------------------------------------------------------
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+__device__ __forceinline__ i32x4 make_rsrc(const void *p, uint32_t bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(p);
+  return i32x4{(int)(uint32_t)a, (int)(uint32_t)(a >> 32), (int)bytes, 0x00020000};
+}
+
+// One 16-byte chunk a lane from rsrc + voff + soff into 64 chunks at dst.
+__device__ __forceinline__ void copy16(i32x4 r, uint8_t *dst, int voff, int soff) {
+  const uint32_t m = (uint32_t)(size_t)(lds_void *)dst;
+  asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(voff), "s"(r), "s"(soff), "{m0}"(m)
+               : "memory");
+}
+
+// This wave's copies have landed, and every wave's.
+__device__ __forceinline__ void step_barrier() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+template <int kTW_, int kTX_, int kWR_, int kWC_>
+struct Tile {
+  static constexpr int kTW = kTW_, kTX = kTX_, kWR = kWR_, kWC = kWC_;
+  static constexpr int kWaves = kWR * kWC, kThreads = 64 * kWaves;
+  static constexpr int kFR = kTW / kWR / 32, kFC = kTX / kWC / 32;  // pieces a wave
+  static constexpr int kStage = (kTW + kTX) * kBlk;                  // LDS bytes a step
+  static constexpr int kCopies = kStage / 1024 / kWaves;             // a wave and step
+  static constexpr int kOutRow = kFR * 64 + 16;  // LDS bytes of a token's bf16 outputs
+  static constexpr int kOutLds = kWaves * 32 * kOutRow;
+  static constexpr int kLds = 2 * kStage > kOutLds ? 2 * kStage : kOutLds;
+  static_assert(kStage % (1024 * kWaves) == 0 && kTW % 8 == 0 && kTX % 8 == 0);
+  static_assert(kLds <= 160 * 1024);
+};
+
+struct LinearArgs {
+  const uint8_t *wcodes, *wscales;
+  XTiles x;
+  int64_t T, m;
+  int C;             // column blocks
+  int R, X;          // 128-row blocks of W and of the tokens
+  int nW, nX;        // tiles
+  void *y;
+};
+
+template <typename TT, int kWFormat, int kXFormat, int kOut>
+__global__ __launch_bounds__(TT::kThreads) void tile_kernel(LinearArgs g) {
+  constexpr int kFR = TT::kFR, kFC = TT::kFC;
+  extern __shared__ uint8_t lds[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+  // workgroups of one XCD (blockIdx mod 8) take a contiguous range of tiles,
+  // token tiles fastest, so that they share rows of W in their L2
+  const int total = g.nW * g.nX;
+  int L = blockIdx.x;
+  if ((total & 7) == 0) L = (L & 7) * (total >> 3) + (L >> 3);
+  const int w0 = L / g.nX * TT::kTW, x0 = L % g.nX * TT::kTX;  // first row and token
+  const int C = g.C;
+
+  // copy roles: piece p = wave kCopies + q is eight tile rows, W's first
+  const int64_t band = (int64_t)C * kTileBytes;  // bytes of 128 rows
+  const int wb0 = w0 >> 7, xb0 = x0 >> 7;
+  const i32x4 wr = make_rsrc(g.wcodes + wb0 * band, 0x7fffffffu);
+  const i32x4 xr = make_rsrc(g.x.codes + xb0 * band, 0x7fffffffu);
+  const int voff = (lane >> 3) * kBlk + (((lane & 7) ^ (lane >> 3)) << 4);
+  int soff[TT::kCopies];
+#pragma unroll
+  for (int q = 0; q < TT::kCopies; ++q) {
+    const int row = 8 * (wave * TT::kCopies + q);
+    const bool isw = row < TT::kTW;
+    const int at = isw ? (w0 & 127) + row : (x0 & 127) + row - TT::kTW;
+    // a tile may reach past the last block: it reads that one again, and what
+    // comes of it is not stored
+    const int blk = min(at >> 7, (isw ? g.R - 1 - wb0 : g.X - 1 - xb0));
+    soff[q] = (int)(blk * band) + (at & 127) * kBlk;
+  }
+  auto issue = [&](int J, int buf) {
+#pragma unroll
+    for (int q = 0; q < TT::kCopies; ++q) {
+      const int p = wave * TT::kCopies + q;
+      copy16(8 * p < TT::kTW ? wr : xr, lds + buf * TT::kStage + p * 1024, voff,
+             soff[q] + J * (int)kTileBytes);
+    }
+  };
+
+  // operands: rows row0 .. of W and tokens tok0 .. of the tile
+  const int row0 = wave / TT::kWC * kFR * 32, tok0 = wave % TT::kWC * kFC * 32;
+  const int arow = row0 + r, brow = TT::kTW + tok0 + r;
+  const int wblk = min((w0 + row0) >> 7, g.R - 1), xblk = min((x0 + tok0) >> 7, g.X - 1);
+  const uint8_t *wsc = g.wscales + (int64_t)wblk * C;
+  const uint32_t *xsc =
+      reinterpret_cast<const uint32_t *>(g.x.scales + (int64_t)xblk * C * kBlk) + r;
+  const int xshift = 8 * (((x0 + tok0) & 127) >> 5);
+
+  v16f acc[kFR][kFC] = {};
+  int sw = wsc[0], sx = (int)(xsc[0] >> xshift);
+  issue(0, 0);
+  for (int J = 0; J < C; ++J) {
+    const int buf = J & 1;
+    step_barrier();
+    const int Jn = min(J + 1, C - 1);
+    const int swn = wsc[Jn], sxn = (int)(xsc[(int64_t)Jn * 32] >> xshift);
+    if (J + 1 < C) issue(J + 1, buf ^ 1);
+    const uint8_t *st = lds + buf * TT::kStage;
+    auto operand = [&](int row, int s) {
+      const uint8_t *p = st + row * kBlk;
+      const int c = 4 * s + 2 * h;
+      const i32x4 lo = *reinterpret_cast<const i32x4 *>(p + ((c ^ (row & 7)) << 4));
+      const i32x4 hi = *reinterpret_cast<const i32x4 *>(p + (((c + 1) ^ (row & 7)) << 4));
+      return v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+    if constexpr (kOut == AF1_SRC_BF16) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        v8i a[kFR], b[kFC];
+#pragma unroll
+        for (int i = 0; i < kFR; ++i) a[i] = operand(arow + 32 * i, s);
+#pragma unroll
+        for (int j = 0; j < kFC; ++j) b[j] = operand(brow + 32 * j, s);
+#pragma unroll
+        for (int i = 0; i < kFR; ++i) {
+          // the byte of a piece's scale is part of the instruction
+          acc[i][0] = mfma_scaled<kWFormat, kXFormat, 0>(a[i], b[0], acc[i][0], sw, sx);
+          if constexpr (kFC > 1)
+            acc[i][1] = mfma_scaled<kWFormat, kXFormat, 1>(a[i], b[1], acc[i][1], sw, sx);
+          if constexpr (kFC > 2) {
+            acc[i][2] = mfma_scaled<kWFormat, kXFormat, 2>(a[i], b[2], acc[i][2], sw, sx);
+            acc[i][3] = mfma_scaled<kWFormat, kXFormat, 3>(a[i], b[3], acc[i][3], sw, sx);
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kFC; ++j) {
+        bf8v b[8];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const v8i c = operand(brow + 32 * j, s);
+          const int lo[4] = {c[0], c[1], c[2], c[3]}, hi[4] = {c[4], c[5], c[6], c[7]};
+          to_bf16<kXFormat>(lo, *reinterpret_cast<bf8v(*)[2]>(b + 4 * s));
+          to_bf16<kXFormat>(hi, *reinterpret_cast<bf8v(*)[2]>(b + 4 * s + 2));
+        }
+        const int e = sw + (sx >> (8 * j) & 255) - 254;
+#pragma unroll
+        for (int i = 0; i < kFR; ++i) {
+          v16f tmp = {};
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            const v8i c = operand(arow + 32 * i, s);
+            const int lo[4] = {c[0], c[1], c[2], c[3]}, hi[4] = {c[4], c[5], c[6], c[7]};
+            bf8v a[4];
+            to_bf16<kWFormat>(lo, *reinterpret_cast<bf8v(*)[2]>(a));
+            to_bf16<kWFormat>(hi, *reinterpret_cast<bf8v(*)[2]>(a + 2));
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              tmp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[q], b[4 * s + q], tmp, 0, 0, 0);
+          }
+#pragma unroll
+          for (int q = 0; q < 16; ++q) acc[i][j][q] += ldexpf(tmp[q], e);
+        }
+      }
+    }
+    sw = swn;
+    sx = sxn;
+  }
+
+  // Outputs.  A lane holds, for its token, four consecutive rows of W in each
+  // four accumulators.
+  if constexpr (kOut == AF1_SRC_F32) {
+    float *y = static_cast<float *>(g.y);
+#pragma unroll
+    for (int j = 0; j < kFC; ++j) {
+      const int64_t t = x0 + tok0 + 32 * j + r;
+      if (t >= g.T) continue;
+#pragma unroll
+      for (int i = 0; i < kFR; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t row = (int64_t)w0 + row0 + 32 * i + 8 * q + 4 * h;
+          float *p = y + t * g.m + row;
+          const v16f &c = acc[i][j];
+          if (row + 4 <= g.m) {
+            Four f{{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]}};
+            *reinterpret_cast<Four *>(p) = f;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (row + e < g.m) p[e] = c[4 * q + e];
+          }
+        }
+    }
+  } else {
+    // through LDS, 32 tokens at a time, so that a token's entries leave in
+    // 16-byte pieces next to each other; each wave uses a region of its own
+    uint16_t *y = static_cast<uint16_t *>(g.y);
+    step_barrier();
+    uint8_t *mine = lds + wave * 32 * TT::kOutRow;
+    constexpr int kLanes = kFR * 4;  // lanes a token
+#pragma unroll
+    for (int j = 0; j < kFC; ++j) {
+#pragma unroll
+      for (int i = 0; i < kFR; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const v16f &c = acc[i][j];
+          const uint32_t lo = pack_bf16(c[4 * q], c[4 * q + 1]);
+          const uint32_t hi = pack_bf16(c[4 * q + 2], c[4 * q + 3]);
+          *reinterpret_cast<uint2 *>(mine + r * TT::kOutRow + (32 * i + 8 * q + 4 * h) * 2) =
+              make_uint2(lo, hi);
+        }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int k = 0; k < kLanes / 2; ++k) {
+        const int tok = k * (64 / kLanes) + lane / kLanes, piece = lane % kLanes;
+        const uint4 v = *reinterpret_cast<const uint4 *>(mine + tok * TT::kOutRow + piece * 16);
+        const int64_t t = x0 + tok0 + 32 * j + tok, row = (int64_t)w0 + row0 + 8 * piece;
+        if (t < g.T && row < g.m) store8_bf16(y + t * g.m + row, g.m - row, v);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
   }
 }
 
@@ -299,6 +508,15 @@ auto with_dense(int t, F &&g) {
   if (t == AF1_SRC_F32) return g(Int<AF1_SRC_F32>{});
   if (t == AF1_SRC_BF16) return g(Int<AF1_SRC_BF16>{});
   return g(Int<AF1_SRC_F16>{});
+}
+
+template <typename TT, int kWFormat, int kXFormat, int kOut>
+hipError_t launch_tiles(LinearArgs g, hipStream_t s) {
+  auto kernel = tile_kernel<TT, kWFormat, kXFormat, kOut>;
+  g.nW = (int)((g.m + TT::kTW - 1) / TT::kTW);
+  g.nX = (int)((g.T + TT::kTX - 1) / TT::kTX);
+  kernel<<<(unsigned)g.nW * (unsigned)g.nX, TT::kThreads, TT::kLds, s>>>(g);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -348,14 +566,12 @@ hipError_t launch_fp8_linear(const af1_fp8_matrix &W, const void *x, int x_dtype
     });
     if (e != hipSuccess) return e;
     return with_format(W.format, [&](auto wf) {
-      const dim3 g((unsigned)((m + 127) / 128), (unsigned)((T + 31) / 32));
+      LinearArgs g{W.codes, W.scales, xt, T, m, (int)blocks_up(n), (int)blocks_up(m),
+                   (int)blocks_up(T), 0, 0, y};
       if (y_dtype == AF1_SRC_F32)
-        linear_kernel<xf.value, wf.value, AF1_SRC_F32>
-            <<<g, 256, 0, s>>>(W.codes, W.scales, xt, T, m, n, y);
-      else
-        linear_kernel<xf.value, wf.value, AF1_SRC_BF16>
-            <<<g, 256, 0, s>>>(W.codes, W.scales, xt, T, m, n, y);
-      return hipGetLastError();
+        return launch_tiles<Tile<128, 128, 2, 2>, wf.value, xf.value, AF1_SRC_F32>(g, s);
+      if (T <= 1024) return launch_tiles<Tile<128, 128, 2, 2>, wf.value, xf.value, AF1_SRC_BF16>(g, s);
+      return launch_tiles<Tile<256, 256, 2, 2>, wf.value, xf.value, AF1_SRC_BF16>(g, s);
     });
   });
 }
