@@ -205,11 +205,11 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const void *x, int64
   if (lane == 0) out.scales[tile * kBlk + (row & 31) * 4 + (row >> 5)] = (uint8_t)(e + 127);
 }
 
-// Sixteen bfloat16 values of sixteen codes, for two matrix instructions.
+// The values of a lane's 32 codes, for four matrix instructions.
 template <int kFormat>
-__device__ __forceinline__ void to_bf16(const int *w, bf8v (&out)[2]) {
+__device__ __forceinline__ void to_bf16(v8i w, bf8v (&out)[4]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 8; ++i) {
     bf2v lo, hi;
     if constexpr (kFormat == AF1_FP8_E4M3) {
       lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.f, false);
@@ -260,22 +260,31 @@ __device__ __forceinline__ void store8_bf16(uint16_t *p, int64_t left, uint4 v) 
 
 // ---------------------------------------------------------------------------
 // Tiled product.  A workgroup of kWR x kWC waves computes kTW rows of W x kTX
-// tokens; a wave kFR x kFC pieces of 32 x 32.  A step is one column block: the
-// tile rows' 128 bytes go from memory straight into LDS (buffer loads with an
-// LDS destination), double-buffered: a step waits for its own copies, meets
-// the other waves once, issues the next step's copies and multiplies.
+// tokens; a wave kFR x kFC pieces of 32 x 32.  A step is half a column block
+// (64 columns).  Its bytes go from memory straight into one of kStages LDS
+// buffers (buffer loads with an LDS destination) and from there into registers
+// one step before they are multiplied, so in step s
+//   buffer s + 1 has landed and is read into registers,
+//   buffers s + 2 .. s + kStages - 1 are on their way, and
+//   buffer s, whose operands are in registers, is filled with step s + kStages.
+// A step meets the other waves once; nothing in it waits for memory that was
+// asked for in the last kStages - 2 steps.  (With two buffers of a whole block
+// each, which hold as many bytes, a step waited for copies issued in the step
+// before: 1289 us where this takes 992 at 128256 x 4096 and 2048 tokens.)
 //
-// LDS holds rows of 128 bytes, eight chunks of 16.  A copy instruction writes
-// 64 consecutive chunks (eight rows), one a lane, and a lane chooses its
-// source: chunk c of row r is kept at position c XOR (r mod 8), so that the
-// operand reads of eight consecutive rows fall in distinct banks.
+// LDS holds rows of 64 bytes, four chunks of 16.  A copy instruction writes 64
+// consecutive chunks (sixteen rows), one a lane, and a lane chooses its
+// source: chunk c of row r is kept at position c XOR (r / 4 mod 4).  The LDS
+// serves a 16-byte read of 64 lanes in groups of sixteen, of which four have
+// equal r mod 4; these then fall in distinct banks (counted: 0.3 conflict
+// cycles a read, against 4.1 with rows of 128 bytes and c XOR (r mod 8)).
 // ---------------------------------------------------------------------------
 
 typedef __attribute__((address_space(3))) void lds_void;
 
-__device__ __forceinline__ i32x4 make_rsrc(const void *p, uint32_t bytes) {
+__device__ __forceinline__ i32x4 make_rsrc(const void *p) {
   const uint64_t a = reinterpret_cast<uint64_t>(p);
-  return i32x4{(int)(uint32_t)a, (int)(uint32_t)(a >> 32), (int)bytes, 0x00020000};
+  return i32x4{(int)(uint32_t)a, (int)(uint32_t)(a >> 32), 0x7fffffff, 0x00020000};
 }
 
 // One 16-byte chunk a lane from rsrc + voff + soff into 64 chunks at dst.
@@ -285,23 +294,38 @@ __device__ __forceinline__ void copy16(i32x4 r, uint8_t *dst, int voff, int soff
                : "memory");
 }
 
-// This wave's copies have landed, and every wave's.
-__device__ __forceinline__ void step_barrier() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+// One dword, or one byte, a lane from the lane's own address into 64 dwords at
+// dst.
+__device__ __forceinline__ void copy4(const void *src, uint8_t *dst) {
+  const uint32_t m = (uint32_t)(size_t)(lds_void *)dst;
+  asm volatile("global_load_lds_dword %0, off" ::"v"(src), "{m0}"(m) : "memory");
+}
+__device__ __forceinline__ void copy1(const void *src, uint8_t *dst) {
+  const uint32_t m = (uint32_t)(size_t)(lds_void *)dst;
+  asm volatile("global_load_lds_ubyte %0, off" ::"v"(src), "{m0}"(m) : "memory");
 }
 
-template <int kTW_, int kTX_, int kWR_, int kWC_>
+// All but kLeft of this wave's copies have landed, its LDS reads are done, and
+// every other wave's too.
+template <int kLeft>
+__device__ __forceinline__ void step_barrier() {
+  static_assert(kLeft >= 0 && kLeft < 64, "vmcnt has six bits");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLeft) : "memory");
+}
+
+template <int kTW_, int kTX_, int kWR_, int kWC_, int kStages_>
 struct Tile {
-  static constexpr int kTW = kTW_, kTX = kTX_, kWR = kWR_, kWC = kWC_;
+  static constexpr int kTW = kTW_, kTX = kTX_, kWR = kWR_, kWC = kWC_, kStages = kStages_;
   static constexpr int kWaves = kWR * kWC, kThreads = 64 * kWaves;
   static constexpr int kFR = kTW / kWR / 32, kFC = kTX / kWC / 32;  // pieces a wave
-  static constexpr int kStage = (kTW + kTX) * kBlk;                  // LDS bytes a step
-  static constexpr int kCopies = kStage / 1024 / kWaves;             // a wave and step
+  static constexpr int kCodes = (kTW + kTX) * 64;      // LDS bytes a step
+  static constexpr int kStage = kCodes + kWaves * 512;  // and the scales', two slots a wave
+  static constexpr int kCopies = kCodes / 1024 / kWaves;  // a wave and step, and two of scales
   static constexpr int kOutRow = kFR * 64 + 16;  // LDS bytes of a token's bf16 outputs
   static constexpr int kOutLds = kWaves * 32 * kOutRow;
-  static constexpr int kLds = 2 * kStage > kOutLds ? 2 * kStage : kOutLds;
-  static_assert(kStage % (1024 * kWaves) == 0 && kTW % 8 == 0 && kTX % 8 == 0);
-  static_assert(kLds <= 160 * 1024);
+  static constexpr int kLds = kStages * kStage > kOutLds ? kStages * kStage : kOutLds;
+  static_assert(kCodes % (1024 * kWaves) == 0 && kTW % 16 == 0 && kTX % 16 == 0);
+  static_assert((kStages & (kStages - 1)) == 0 && kLds <= 160 * 1024);
 };
 
 struct LinearArgs {
@@ -316,7 +340,7 @@ struct LinearArgs {
 
 template <typename TT, int kWFormat, int kXFormat, int kOut>
 __global__ __launch_bounds__(TT::kThreads) void tile_kernel(LinearArgs g) {
-  constexpr int kFR = TT::kFR, kFC = TT::kFC;
+  constexpr int kFR = TT::kFR, kFC = TT::kFC, kS = TT::kStages;
   extern __shared__ uint8_t lds[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
@@ -328,16 +352,16 @@ __global__ __launch_bounds__(TT::kThreads) void tile_kernel(LinearArgs g) {
   const int w0 = L / g.nX * TT::kTW, x0 = L % g.nX * TT::kTX;  // first row and token
   const int C = g.C;
 
-  // copy roles: piece p = wave kCopies + q is eight tile rows, W's first
+  // copy roles: piece p = wave kCopies + q is sixteen tile rows, W's first
   const int64_t band = (int64_t)C * kTileBytes;  // bytes of 128 rows
   const int wb0 = w0 >> 7, xb0 = x0 >> 7;
-  const i32x4 wr = make_rsrc(g.wcodes + wb0 * band, 0x7fffffffu);
-  const i32x4 xr = make_rsrc(g.x.codes + xb0 * band, 0x7fffffffu);
-  const int voff = (lane >> 3) * kBlk + (((lane & 7) ^ (lane >> 3)) << 4);
+  const i32x4 wr = make_rsrc(g.wcodes + wb0 * band);
+  const i32x4 xr = make_rsrc(g.x.codes + xb0 * band);
+  const int voff = (lane >> 2) * kBlk + (((lane & 3) ^ (lane >> 4)) << 4);
   int soff[TT::kCopies];
 #pragma unroll
   for (int q = 0; q < TT::kCopies; ++q) {
-    const int row = 8 * (wave * TT::kCopies + q);
+    const int row = 16 * (wave * TT::kCopies + q);
     const bool isw = row < TT::kTW;
     const int at = isw ? (w0 & 127) + row : (x0 & 127) + row - TT::kTW;
     // a tile may reach past the last block: it reads that one again, and what
@@ -345,95 +369,132 @@ __global__ __launch_bounds__(TT::kThreads) void tile_kernel(LinearArgs g) {
     const int blk = min(at >> 7, (isw ? g.R - 1 - wb0 : g.X - 1 - xb0));
     soff[q] = (int)(blk * band) + (at & 127) * kBlk;
   }
-  auto issue = [&](int J, int buf) {
+  // operands: rows row0 .. of W and tokens tok0 .. of the tile
+  const int row0 = wave / TT::kWC * kFR * 32, tok0 = wave % TT::kWC * kFC * 32;
+  const int wblk = min((w0 + row0) >> 7, g.R - 1), xblk = min((x0 + tok0) >> 7, g.X - 1);
+  // scales: the tokens' dwords and W's byte of a block, each lane its own
+  const uint8_t *wsc = g.wscales + (int64_t)wblk * C;
+  const uint8_t *xsc = g.x.scales + (int64_t)xblk * C * kBlk + r * 4;
+  // copy k of step s: codes, then the scales
+  constexpr int kCopies = TT::kCopies + 2;
+  auto copy = [&](int s, int k) {
+    uint8_t *st = lds + (s & (kS - 1)) * TT::kStage;
+    const int J = s >> 1, p = wave * TT::kCopies + k;
+    if (k < TT::kCopies)
+      copy16(16 * p < TT::kTW ? wr : xr, st + p * 1024, voff,
+             soff[k < TT::kCopies ? k : 0] + J * (int)kTileBytes + (s & 1) * 64);
+    else if (k == TT::kCopies)
+      copy4(xsc + J * kBlk, st + TT::kCodes + wave * 512);
+    else
+      copy1(wsc + J, st + TT::kCodes + wave * 512 + 256);
+  };
+
+  const int xshift = 8 * (((x0 + tok0) & 127) >> 5);
+  struct Operands {
+    v8i a[kFR], b[kFC];
+    int sw, sx;
+  };
+  // piece k of step s: W's, the tokens', the scales
+  constexpr int kReads = kFR + kFC + 1;
+  const int lo = ((2 * h) ^ (r >> 2 & 3)) << 4, hi = lo ^ 16;
+  auto read = [&](int s, int k, Operands &o) {
+    const uint8_t *st = lds + (s & (kS - 1)) * TT::kStage;
+    if (k == 0) {
+      const uint32_t *sc = reinterpret_cast<const uint32_t *>(st + TT::kCodes + wave * 512);
+      o.sx = (int)(sc[r] >> xshift);
+      o.sw = (int)sc[64 + lane];
+      return;
+    }
+    const int piece = k - 1;
+    const int row = piece < kFR ? row0 + 32 * piece : TT::kTW + tok0 + 32 * (piece - kFR);
+    const uint8_t *p = st + (row + r) * 64;
+    const i32x4 u = *reinterpret_cast<const i32x4 *>(p + lo);
+    const i32x4 v = *reinterpret_cast<const i32x4 *>(p + hi);
+    (piece < kFR ? o.a[piece < kFR ? piece : 0] : o.b[piece < kFR ? 0 : piece - kFR]) =
+        v8i{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+  };
+
+  v16f acc[kFR][kFC] = {};
+  v16f tmp[kFR][kFC];  // a block's sums, for outputs in fp32
+  auto product = [&](const Operands &o, bool second, int i, int j) {
+    if constexpr (kOut == AF1_SRC_BF16) {
+      // which byte holds a piece's scale is part of the instruction
+      if (j == 0) acc[i][0] = mfma_scaled<kWFormat, kXFormat, 0>(o.a[i], o.b[0], acc[i][0], o.sw, o.sx);
+      if constexpr (kFC > 1)
+        if (j == 1)
+          acc[i][1] = mfma_scaled<kWFormat, kXFormat, 1>(o.a[i], o.b[1], acc[i][1], o.sw, o.sx);
+      if constexpr (kFC > 2) {
+        if (j == 2)
+          acc[i][2] = mfma_scaled<kWFormat, kXFormat, 2>(o.a[i], o.b[2], acc[i][2], o.sw, o.sx);
+        if (j == 3)
+          acc[i][3] = mfma_scaled<kWFormat, kXFormat, 3>(o.a[i], o.b[3], acc[i][3], o.sw, o.sx);
+      }
+    } else {
+      bf8v a[4], b[4];
+      to_bf16<kWFormat>(o.a[i], a);
+      to_bf16<kXFormat>(o.b[j], b);
+      v16f t = second ? tmp[i][j] : v16f{};
 #pragma unroll
-    for (int q = 0; q < TT::kCopies; ++q) {
-      const int p = wave * TT::kCopies + q;
-      copy16(8 * p < TT::kTW ? wr : xr, lds + buf * TT::kStage + p * 1024, voff,
-             soff[q] + J * (int)kTileBytes);
+      for (int q = 0; q < 4; ++q)
+        t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[q], b[q], t, 0, 0, 0);
+      tmp[i][j] = t;
+      if (second) {
+        const int e = o.sw + (o.sx >> (8 * j) & 255) - 254;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[i][j][q] += ldexpf(t[q], e);
+      }
     }
   };
 
-  // operands: rows row0 .. of W and tokens tok0 .. of the tile
-  const int row0 = wave / TT::kWC * kFR * 32, tok0 = wave % TT::kWC * kFC * 32;
-  const int arow = row0 + r, brow = TT::kTW + tok0 + r;
-  const int wblk = min((w0 + row0) >> 7, g.R - 1), xblk = min((x0 + tok0) >> 7, g.X - 1);
-  const uint8_t *wsc = g.wscales + (int64_t)wblk * C;
-  const uint32_t *xsc =
-      reinterpret_cast<const uint32_t *>(g.x.scales + (int64_t)xblk * C * kBlk) + r;
-  const int xshift = 8 * (((x0 + tok0) & 127) >> 5);
-
-  v16f acc[kFR][kFC] = {};
-  int sw = wsc[0], sx = (int)(xsc[0] >> xshift);
-  issue(0, 0);
-  for (int J = 0; J < C; ++J) {
-    const int buf = J & 1;
-    step_barrier();
-    const int Jn = min(J + 1, C - 1);
-    const int swn = wsc[Jn], sxn = (int)(xsc[(int64_t)Jn * 32] >> xshift);
-    if (J + 1 < C) issue(J + 1, buf ^ 1);
-    const uint8_t *st = lds + buf * TT::kStage;
-    auto operand = [&](int row, int s) {
-      const uint8_t *p = st + row * kBlk;
-      const int c = 4 * s + 2 * h;
-      const i32x4 lo = *reinterpret_cast<const i32x4 *>(p + ((c ^ (row & 7)) << 4));
-      const i32x4 hi = *reinterpret_cast<const i32x4 *>(p + (((c + 1) ^ (row & 7)) << 4));
-      return v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    };
-    if constexpr (kOut == AF1_SRC_BF16) {
+  // Step s: its products, and between them the copies of step s + kStages and
+  // the reads of step s + 1, the reads in the first half so that the barrier
+  // does not wait for them.  A burst of copies in front of the products keeps
+  // the wave's issue waiting behind the other waves' bursts.
+  constexpr int kProducts = kFR * kFC;
+  auto step = [&](int s, const Operands &o, Operands &next, bool second, bool more, bool last) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        v8i a[kFR], b[kFC];
+    for (int p = 0; p < kProducts; ++p) {
+      constexpr int kHalf = kProducts > 1 ? kProducts / 2 : 1;
+      if (!last && p < kHalf)
 #pragma unroll
-        for (int i = 0; i < kFR; ++i) a[i] = operand(arow + 32 * i, s);
+        for (int k = p * kReads / kHalf; k < (p + 1) * kReads / kHalf; ++k) read(s + 1, k, next);
+      if (more)
 #pragma unroll
-        for (int j = 0; j < kFC; ++j) b[j] = operand(brow + 32 * j, s);
-#pragma unroll
-        for (int i = 0; i < kFR; ++i) {
-          // the byte of a piece's scale is part of the instruction
-          acc[i][0] = mfma_scaled<kWFormat, kXFormat, 0>(a[i], b[0], acc[i][0], sw, sx);
-          if constexpr (kFC > 1)
-            acc[i][1] = mfma_scaled<kWFormat, kXFormat, 1>(a[i], b[1], acc[i][1], sw, sx);
-          if constexpr (kFC > 2) {
-            acc[i][2] = mfma_scaled<kWFormat, kXFormat, 2>(a[i], b[2], acc[i][2], sw, sx);
-            acc[i][3] = mfma_scaled<kWFormat, kXFormat, 3>(a[i], b[3], acc[i][3], sw, sx);
-          }
-        }
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < kFC; ++j) {
-        bf8v b[8];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const v8i c = operand(brow + 32 * j, s);
-          const int lo[4] = {c[0], c[1], c[2], c[3]}, hi[4] = {c[4], c[5], c[6], c[7]};
-          to_bf16<kXFormat>(lo, *reinterpret_cast<bf8v(*)[2]>(b + 4 * s));
-          to_bf16<kXFormat>(hi, *reinterpret_cast<bf8v(*)[2]>(b + 4 * s + 2));
-        }
-        const int e = sw + (sx >> (8 * j) & 255) - 254;
-#pragma unroll
-        for (int i = 0; i < kFR; ++i) {
-          v16f tmp = {};
-#pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            const v8i c = operand(arow + 32 * i, s);
-            const int lo[4] = {c[0], c[1], c[2], c[3]}, hi[4] = {c[4], c[5], c[6], c[7]};
-            bf8v a[4];
-            to_bf16<kWFormat>(lo, *reinterpret_cast<bf8v(*)[2]>(a));
-            to_bf16<kWFormat>(hi, *reinterpret_cast<bf8v(*)[2]>(a + 2));
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              tmp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[q], b[4 * s + q], tmp, 0, 0, 0);
-          }
-#pragma unroll
-          for (int q = 0; q < 16; ++q) acc[i][j][q] += ldexpf(tmp[q], e);
-        }
-      }
+        for (int k = p * kCopies / kProducts; k < (p + 1) * kCopies / kProducts; ++k)
+          copy(s + kS, k);
+      product(o, second, p / kFC, p % kFC);
+      if constexpr (kOut == AF1_SRC_BF16) __builtin_amdgcn_sched_barrier(0);
     }
-    sw = swn;
-    sx = sxn;
+  };
+
+  // copies of the steps behind the next one
+  constexpr int kAhead = (kS - 2) * kCopies;
+  const int steps = 2 * C;
+  for (int s = 0; s < min(kS, steps); ++s)
+#pragma unroll
+    for (int k = 0; k < kCopies; ++k) copy(s, k);
+  step_barrier<0>();
+  Operands o0, o1;
+#pragma unroll
+  for (int k = 0; k < kReads; ++k) read(0, k, o0);
+  int J = 0;
+  for (; 2 * J + 1 + kS < steps; ++J) {
+    step_barrier<kAhead>();
+    step(2 * J, o0, o1, false, true, false);
+    step_barrier<kAhead>();
+    step(2 * J + 1, o1, o0, true, true, false);
   }
+  // nothing more to copy: what is left has been on its way for long
+  for (; J < C - 1; ++J) {
+    step_barrier<0>();
+    step(2 * J, o0, o1, false, false, false);
+    step_barrier<0>();
+    step(2 * J + 1, o1, o0, true, false, false);
+  }
+  step_barrier<0>();
+  step(2 * J, o0, o1, false, false, false);
+  step_barrier<0>();
+  step(2 * J + 1, o1, o0, true, false, true);
 
   // Outputs.  A lane holds, for its token, four consecutive rows of W in each
   // four accumulators.
@@ -464,7 +525,7 @@ __global__ __launch_bounds__(TT::kThreads) void tile_kernel(LinearArgs g) {
     // through LDS, 32 tokens at a time, so that a token's entries leave in
     // 16-byte pieces next to each other; each wave uses a region of its own
     uint16_t *y = static_cast<uint16_t *>(g.y);
-    step_barrier();
+    step_barrier<0>();
     uint8_t *mine = lds + wave * 32 * TT::kOutRow;
     constexpr int kLanes = kFR * 4;  // lanes a token
 #pragma unroll
@@ -569,9 +630,9 @@ hipError_t launch_fp8_linear(const af1_fp8_matrix &W, const void *x, int x_dtype
       LinearArgs g{W.codes, W.scales, xt, T, m, (int)blocks_up(n), (int)blocks_up(m),
                    (int)blocks_up(T), 0, 0, y};
       if (y_dtype == AF1_SRC_F32)
-        return launch_tiles<Tile<128, 128, 2, 2>, wf.value, xf.value, AF1_SRC_F32>(g, s);
-      if (T <= 1024) return launch_tiles<Tile<128, 128, 2, 2>, wf.value, xf.value, AF1_SRC_BF16>(g, s);
-      return launch_tiles<Tile<256, 256, 2, 2>, wf.value, xf.value, AF1_SRC_BF16>(g, s);
+        return launch_tiles<Tile<128, 128, 2, 2, 4>, wf.value, xf.value, AF1_SRC_F32>(g, s);
+      if (T <= 1024) return launch_tiles<Tile<128, 128, 2, 2, 4>, wf.value, xf.value, AF1_SRC_BF16>(g, s);
+      return launch_tiles<Tile<256, 256, 2, 2, 4>, wf.value, xf.value, AF1_SRC_BF16>(g, s);
     });
   });
 }
