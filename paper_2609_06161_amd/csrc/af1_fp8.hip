@@ -9,38 +9,22 @@
 // outputs over 64 (128) columns; a lane's operand is 32 bytes of one row.
 // Which columns those are is free as long as both operands agree, since all of
 // a block's columns share one scale.
-#include "af1_device.h"
+#include "af1_head_device.h"
 #include "af1_head_internal.h"
 
 namespace af1h {
 namespace {
 
-using af1::bf16_to_f32;
-using af1::f16_to_f32;
 using af1::f32_to_bf16;
-using af1::f32_to_f16;
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
 
 constexpr int64_t kTileBytes = kBlk * kBlk;
-
-template <int kType>
-__device__ __forceinline__ float load_dense(const void *p, int64_t i) {
-  if constexpr (kType == AF1_SRC_F32) return static_cast<const float *>(p)[i];
-  if constexpr (kType == AF1_SRC_BF16) return bf16_to_f32(static_cast<const uint16_t *>(p)[i]);
-  return f16_to_f32(static_cast<const uint16_t *>(p)[i]);
-}
-
-template <int kType>
-__device__ __forceinline__ void store_dense(void *p, int64_t i, float v) {
-  if constexpr (kType == AF1_SRC_F32) static_cast<float *>(p)[i] = v;
-  if constexpr (kType == AF1_SRC_BF16) static_cast<uint16_t *>(p)[i] = f32_to_bf16(v);
-  if constexpr (kType == AF1_SRC_F16) static_cast<uint16_t *>(p)[i] = f32_to_f16(v);
-}
 
 // |x| of a finite entry, 0 for the others: what a block's scale is chosen from.
 __device__ __forceinline__ float finite_abs(float x) {
@@ -88,75 +72,108 @@ __device__ __forceinline__ float decode(uint32_t w) {
 // Quantisation, reading back, transposition: one workgroup a tile.
 // ---------------------------------------------------------------------------
 
-// Thread t of 256 holds row t / 2, columns 64 (t % 2) .. + 63 of the tile.
-template <int kType, int kFormat>
-__global__ __launch_bounds__(256) void quantize_kernel(const void *src, int64_t rows, int64_t cols,
-                                                       uint8_t *codes, uint8_t *scales) {
-  __shared__ float wmax[4];
-  const int64_t C = (cols + kBlk - 1) / kBlk, tile = blockIdx.x;
-  const int64_t r0 = tile / C * kBlk, c0 = tile % C * kBlk;
-  const int t = threadIdx.x;
-  const int64_t row = r0 + (t >> 1), col = c0 + (t & 1) * 64;
-  float v[64], amax = 0.f;
-#pragma unroll
-  for (int j = 0; j < 64; ++j) {
-    v[j] = row < rows && col + j < cols ? load_dense<kType>(src, row * cols + col + j) : 0.f;
-    amax = fmaxf(amax, finite_abs(v[j]));
-  }
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 64));
-  if ((t & 63) == 0) wmax[t >> 6] = amax;
-  __syncthreads();
-  amax = fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3]));
-  const int e = block_exponent<kFormat>(amax);
-  const float inv = pow2(-e);
-  uint4 *dst = reinterpret_cast<uint4 *>(codes + tile * kTileBytes + t * 64);
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float *p = v + 16 * q + 4 * i;
-      w[i] = encode4<kFormat>(p[0] * inv, p[1] * inv, p[2] * inv, p[3] * inv);
-    }
-    dst[q] = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-  if (t == 0) scales[tile] = (uint8_t)(e + 127);
+// Codes of eight values at 2^-e.
+template <int kFormat>
+__device__ __forceinline__ uint2 encode8(const float (&v)[8], float inv) {
+  return make_uint2(encode4<kFormat>(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
+                    encode4<kFormat>(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
 }
 
-template <int kType, int kFormat>
+template <typename D, int kFormat>
+__global__ __launch_bounds__(256) void quantize_kernel(const typename D::raw *src, int64_t rows,
+                                                       int64_t cols, uint8_t *codes,
+                                                       uint8_t *scales, int64_t tiles) {
+  __shared__ float wmax[2][4];
+  const int64_t C = (cols + kBlk - 1) / kBlk;
+  // thread t holds chunk t % 16 of rows t / 16 + 16 q
+  const int t = threadIdx.x, r = t >> 4, k = t & 15;
+  int turn = 0;
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x, turn ^= 1) {
+    const int64_t r0 = tile / C * kBlk + r, left = cols - tile % C * kBlk;
+    const typename D::raw *at = src + r0 * cols + tile % C * kBlk;
+    float v[8][8], amax = 0.f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      if (r0 + 16 * q < rows) {
+        load8<D>(at + 16 * q * cols, k, left, 0.f, v[q]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[q][i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_abs(v[q][i]));
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 64));
+    if ((t & 63) == 0) wmax[turn][t >> 6] = amax;
+    __syncthreads();
+    const float *w = wmax[turn];
+    const int e = block_exponent<kFormat>(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])));
+    const float inv = pow2(-e);
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      *reinterpret_cast<uint2 *>(codes + tile * kTileBytes + (r + 16 * q) * kBlk + 8 * k) =
+          encode8<kFormat>(v[q], inv);
+    if (t == 0) scales[tile] = (uint8_t)(e + 127);
+  }
+}
+
+template <typename D, int kFormat>
 __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t *codes,
                                                          const uint8_t *scales, int64_t rows,
-                                                         int64_t cols, void *dst) {
-  const int64_t C = (cols + kBlk - 1) / kBlk, tile = blockIdx.x;
-  const int t = threadIdx.x;
-  const int64_t row = tile / C * kBlk + (t >> 1), col = tile % C * kBlk + (t & 1) * 64;
-  if (row >= rows) return;
-  const float scale = pow2((int)scales[tile] - 127);
-  const uint32_t *src = reinterpret_cast<const uint32_t *>(codes + tile * kTileBytes + t * 64);
-#pragma unroll 4
-  for (int q = 0; q < 16; ++q) {
-    const uint32_t w = src[q];
-    const float v[4] = {decode<kFormat, 0>(w), decode<kFormat, 1>(w), decode<kFormat, 2>(w),
-                        decode<kFormat, 3>(w)};
+                                                         int64_t cols, typename D::raw *dst,
+                                                         int64_t tiles) {
+  const int64_t C = (cols + kBlk - 1) / kBlk;
+  const int r = threadIdx.x >> 4, k = threadIdx.x & 15;
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const int64_t r0 = tile / C * kBlk + r, left = cols - tile % C * kBlk;
+    typename D::raw *at = dst + r0 * cols + tile % C * kBlk;
+    const float scale = pow2((int)scales[tile] - 127);
+    uint2 w[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (col + 4 * q + i < cols) store_dense<kType>(dst, row * cols + col + 4 * q + i, v[i] * scale);
+    for (int q = 0; q < 8; ++q)
+      w[q] = *reinterpret_cast<const uint2 *>(codes + tile * kTileBytes + (r + 16 * q) * kBlk + 8 * k);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      if (r0 + 16 * q >= rows) continue;
+      const float v[8] = {
+          decode<kFormat, 0>(w[q].x) * scale, decode<kFormat, 1>(w[q].x) * scale,
+          decode<kFormat, 2>(w[q].x) * scale, decode<kFormat, 3>(w[q].x) * scale,
+          decode<kFormat, 0>(w[q].y) * scale, decode<kFormat, 1>(w[q].y) * scale,
+          decode<kFormat, 2>(w[q].y) * scale, decode<kFormat, 3>(w[q].y) * scale};
+      store8<D>(at + 16 * q * cols, k, left, v);
+    }
   }
 }
 
+// Rows of 132 bytes in LDS: a column's bytes lie 33 banks apart.
 __global__ __launch_bounds__(256) void transpose_tiles_kernel(const uint8_t *codes,
                                                               const uint8_t *scales, int64_t R,
                                                               int64_t C, uint8_t *codesT,
                                                               uint8_t *scalesT) {
-  __shared__ uint8_t tile[kBlk][kBlk + 4];
-  const int64_t i = blockIdx.x / C, j = blockIdx.x % C;
-  const uint8_t *src = codes + (int64_t)blockIdx.x * kTileBytes;
-  uint8_t *dst = codesT + (j * R + i) * kTileBytes;
-  for (int b = threadIdx.x; b < kTileBytes; b += 256) tile[b >> 7][b & 127] = src[b];
-  __syncthreads();
-  for (int b = threadIdx.x; b < kTileBytes; b += 256) dst[b] = tile[b & 127][b >> 7];
-  if (threadIdx.x == 0) scalesT[j * R + i] = scales[blockIdx.x];
+  __shared__ uint8_t lds[kBlk * (kBlk + 4)];
+  for (int64_t tile = blockIdx.x; tile < R * C; tile += gridDim.x) {
+    const int64_t i = tile / C, j = tile % C;
+    const uint32_t *src = reinterpret_cast<const uint32_t *>(codes + tile * kTileBytes);
+    uint32_t *dst = reinterpret_cast<uint32_t *>(codesT + (j * R + i) * kTileBytes);
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      const int w = threadIdx.x + 256 * q;
+      *reinterpret_cast<uint32_t *>(lds + (w >> 5) * (kBlk + 4) + (w & 31) * 4) = src[w];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      // word w of the result: row w / 32, columns 4 (w mod 32) ..
+      const int w = threadIdx.x + 256 * q, row = w >> 5, col = (w & 31) * 4;
+      uint32_t v = 0;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) v |= (uint32_t)lds[(col + b) * (kBlk + 4) + row] << (8 * b);
+      dst[w] = v;
+    }
+    if (threadIdx.x == 0) scalesT[j * R + i] = scales[tile];
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -178,31 +195,27 @@ __host__ __device__ inline XTiles x_tiles(void *ws, int64_t n, int64_t T) {
 }
 
 // Sixteen lanes a token and column block, eight columns a lane.
-template <int kType, int kFormat>
-__global__ __launch_bounds__(256) void quantize_rows_kernel(const void *x, int64_t T, int64_t n,
-                                                            XTiles out) {
+template <typename D, int kFormat>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const typename D::raw *x, int64_t T,
+                                                            int64_t n, XTiles out) {
   const int64_t C = (n + kBlk - 1) / kBlk;
-  const int64_t piece = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  const int lane = threadIdx.x & 15;
-  const int64_t t = piece / C, J = piece % C;
-  if (t >= T) return;  // the sixteen lanes together
-  const int64_t col = J * kBlk + lane * 8;
-  float v[8], amax = 0.f;
+  const int k = threadIdx.x & 15;
+  for (int64_t piece = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); piece < T * C;
+       piece += (int64_t)gridDim.x * 16) {
+    const int64_t t = piece / C, J = piece % C;
+    float v[8], amax = 0.f;
+    load8<D>(x + t * n + J * kBlk, k, n - J * kBlk, 0.f, v);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    v[i] = col + i < n ? load_dense<kType>(x, t * n + col + i) : 0.f;
-    amax = fmaxf(amax, finite_abs(v[i]));
+    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_abs(v[i]));
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 16));
+    const int e = block_exponent<kFormat>(amax);
+    const int64_t tile = t / kBlk * C + J;
+    const int row = (int)(t % kBlk);
+    *reinterpret_cast<uint2 *>(out.codes + tile * kTileBytes + row * kBlk + k * 8) =
+        encode8<kFormat>(v, pow2(-e));
+    if (k == 0) out.scales[tile * kBlk + (row & 31) * 4 + (row >> 5)] = (uint8_t)(e + 127);
   }
-#pragma unroll
-  for (int off = 8; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 16));
-  const int e = block_exponent<kFormat>(amax);
-  const float inv = pow2(-e);
-  const int64_t tile = t / kBlk * C + J;
-  const int row = (int)(t % kBlk);
-  *reinterpret_cast<uint2 *>(out.codes + tile * kTileBytes + row * kBlk + lane * 8) =
-      make_uint2(encode4<kFormat>(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
-                 encode4<kFormat>(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
-  if (lane == 0) out.scales[tile * kBlk + (row & 31) * 4 + (row >> 5)] = (uint8_t)(e + 127);
 }
 
 // The values of a lane's 32 codes, for four matrix instructions.
@@ -553,6 +566,177 @@ __global__ __launch_bounds__(TT::kThreads) void tile_kernel(LinearArgs g) {
   }
 }
 
+// ---------------------------------------------------------------------------
+// Few tokens.  The weight is read once whatever the tokens, so this form is
+// about reading it: a workgroup computes 16 kFR rows of W for up to 16 kNT
+// tokens, its waves take every kWaves-th column block, each streams its rows'
+// codes from memory straight into operands (lane q of a row's four: 16 columns
+// at 16 q and 16 at 64 + q 16, so that one load covers 64 bytes of a row), and
+// the waves' sums are added in LDS in the waves' order.  Up to 16 tokens a
+// wave rounds its own blocks of x to 8 bits in registers, which is one launch
+// and no workspace.  More tokens are rounded by a launch of their own.
+// ---------------------------------------------------------------------------
+
+struct FewArgs {
+  const uint8_t *wcodes, *wscales;
+  const void *x;   // dense, or
+  XTiles xt;       // rounded
+  int T;
+  int64_t m, n;
+  void *y;
+};
+
+// Where a lane's 32 operand columns come from: 16 at k 16, and 16 at 64 + k 16.
+struct RowCodes {
+  i32x4 lo, hi;
+};
+__device__ __forceinline__ v8i operand(const RowCodes &c) {
+  return v8i{c.lo[0], c.lo[1], c.lo[2], c.lo[3], c.hi[0], c.hi[1], c.hi[2], c.hi[3]};
+}
+
+template <typename D>
+struct DenseRow {
+  Eight<typename D::raw> v[4];
+};
+
+template <typename D, int kXFormat, int kWFormat, int kOut, int kFR, int kNT, int kWaves>
+__global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs g) {
+  constexpr bool kDense = kNT == 1;
+  extern __shared__ float sums[];  // [kWaves][kFR][kNT][64][4]
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+  const int64_t n = g.n;
+  const int C = (int)((n + kBlk - 1) / kBlk);
+  const int64_t row0 = (int64_t)blockIdx.x * 16 * kFR;
+  const uint8_t *w = g.wcodes + row0 / kBlk * C * kTileBytes + (row0 % kBlk + r) * kBlk + q * 16;
+  const uint8_t *wsc = g.wscales + row0 / kBlk * C;
+  const typename D::raw *xr = static_cast<const typename D::raw *>(g.x) + (int64_t)r * n + q * 16;
+
+  struct Block {
+    RowCodes w[kFR];
+    int sw;
+    DenseRow<D> d;         // kDense
+    RowCodes x[kNT];       // otherwise
+    int sx[kNT];
+  };
+  auto load = [&](int J, Block &b) {
+#pragma unroll
+    for (int i = 0; i < kFR; ++i) {
+      const i32x4 *p = reinterpret_cast<const i32x4 *>(w + J * kTileBytes + i * 16 * kBlk);
+      b.w[i] = RowCodes{p[0], p[4]};
+    }
+    b.sw = wsc[J];
+    if constexpr (kDense) {
+      const typename D::raw *p = xr + (int64_t)J * kBlk;
+      const int64_t left = n - (int64_t)J * kBlk - q * 16;  // columns from here to the end
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int at = (c & 1) * 8 + (c >> 1) * 64;
+        if (r < g.T && at + 8 <= left) {
+          b.d.v[c] = *reinterpret_cast<const Eight<typename D::raw> *>(p + at);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            b.d.v[c].v[i] = r < g.T && at + i < left ? p[at + i] : (typename D::raw)0;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < kNT; ++t) {
+        const int row = 16 * t + r;
+        const i32x4 *p = reinterpret_cast<const i32x4 *>(g.xt.codes + J * kTileBytes + row * kBlk + q * 16);
+        b.x[t] = RowCodes{p[0], p[4]};
+        b.sx[t] = g.xt.scales[J * kBlk + (row & 31) * 4 + (row >> 5)];
+      }
+    }
+  };
+
+  v4f acc[kFR][kNT] = {};
+  auto multiply = [&](Block &b) {
+    if constexpr (kDense) {
+      float v[4][8], amax = 0.f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        widen<D>(b.d.v[c], v[c]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_abs(v[c][i]));
+      }
+      // the token's four lanes
+      amax = fmaxf(amax, __shfl_xor(amax, 16, 64));
+      amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
+      const int e = block_exponent<kXFormat>(amax);
+      const float inv = pow2(-e);
+      const uint2 c0 = encode8<kXFormat>(v[0], inv), c1 = encode8<kXFormat>(v[1], inv);
+      const uint2 c2 = encode8<kXFormat>(v[2], inv), c3 = encode8<kXFormat>(v[3], inv);
+      b.x[0] = RowCodes{i32x4{(int)c0.x, (int)c0.y, (int)c1.x, (int)c1.y},
+                        i32x4{(int)c2.x, (int)c2.y, (int)c3.x, (int)c3.y}};
+      b.sx[0] = e + 127;
+    }
+    if constexpr (kOut == AF1_SRC_BF16) {
+#pragma unroll
+      for (int i = 0; i < kFR; ++i)
+#pragma unroll
+        for (int t = 0; t < kNT; ++t)
+          acc[i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+              operand(b.w[i]), operand(b.x[t]), acc[i][t], kWFormat, kXFormat, 0, b.sw, 0, b.sx[t]);
+    } else {
+      bf8v xb[kNT][4];
+#pragma unroll
+      for (int t = 0; t < kNT; ++t) to_bf16<kXFormat>(operand(b.x[t]), xb[t]);
+#pragma unroll
+      for (int i = 0; i < kFR; ++i) {
+        bf8v a[4];
+        to_bf16<kWFormat>(operand(b.w[i]), a);
+#pragma unroll
+        for (int t = 0; t < kNT; ++t) {
+          v4f s = {};
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[k], xb[t][k], s, 0, 0, 0);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) acc[i][t][k] += ldexpf(s[k], b.sw + b.sx[t] - 254);
+        }
+      }
+    }
+  };
+
+  // the next block is on its way while this one is multiplied
+  Block b0, b1;
+  int J = wave;
+  if (J < C) load(J, b0);
+  while (J < C) {
+    if (J + kWaves < C) load(J + kWaves, b1);
+    multiply(b0);
+    J += kWaves;
+    if (J >= C) break;
+    if (J + kWaves < C) load(J + kWaves, b0);
+    multiply(b1);
+    J += kWaves;
+  }
+
+  constexpr int kPiece = 256;  // sums of a 16 x 16 piece
+#pragma unroll
+  for (int i = 0; i < kFR; ++i)
+#pragma unroll
+    for (int t = 0; t < kNT; ++t)
+      *reinterpret_cast<v4f *>(sums + ((wave * kFR + i) * kNT + t) * kPiece + lane * 4) = acc[i][t];
+  __syncthreads();
+  // entry o: row o mod 16 kFR of the token o / 16 kFR
+  for (int o = threadIdx.x; o < 16 * kFR * g.T; o += 64 * kWaves) {
+    const int row = o % (16 * kFR), t = o / (16 * kFR);
+    if (row0 + row >= g.m) continue;
+    const int at = ((row >> 4) * kNT + (t >> 4)) * kPiece + ((row & 15) >> 2) * 64 + (t & 15) * 4 + (row & 3);
+    float s = sums[at];
+#pragma unroll
+    for (int k = 1; k < kWaves; ++k) s += sums[at + k * kFR * kNT * kPiece];
+    const int64_t out = (int64_t)t * g.m + row0 + row;
+    if constexpr (kOut == AF1_SRC_F32)
+      static_cast<float *>(g.y)[out] = s;
+    else
+      static_cast<uint16_t *>(g.y)[out] = f32_to_bf16(s);
+  }
+}
+
 template <int kV>
 struct Int {
   static constexpr int value = kV;
@@ -564,13 +748,6 @@ auto with_format(int f, F &&g) {
   return g(Int<AF1_FP8_E5M2>{});
 }
 
-template <typename F>
-auto with_dense(int t, F &&g) {
-  if (t == AF1_SRC_F32) return g(Int<AF1_SRC_F32>{});
-  if (t == AF1_SRC_BF16) return g(Int<AF1_SRC_BF16>{});
-  return g(Int<AF1_SRC_F16>{});
-}
-
 template <typename TT, int kWFormat, int kXFormat, int kOut>
 hipError_t launch_tiles(LinearArgs g, hipStream_t s) {
   auto kernel = tile_kernel<TT, kWFormat, kXFormat, kOut>;
@@ -580,25 +757,49 @@ hipError_t launch_tiles(LinearArgs g, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <typename D, int kXFormat, int kWFormat, int kOut, int kFR, int kNT>
+hipError_t launch_few(const FewArgs &g, hipStream_t s) {
+  constexpr int kWaves = 8;
+  constexpr int kLds = kWaves * kFR * kNT * 1024;
+  few_kernel<D, kXFormat, kWFormat, kOut, kFR, kNT, kWaves>
+      <<<(unsigned)((g.m + 16 * kFR - 1) / (16 * kFR)), 64 * kWaves, kLds, s>>>(g);
+  return hipGetLastError();
+}
+
+// Strips a workgroup: more of them share an operand of x, fewer fill the device.
+template <typename D, int kXFormat, int kWFormat, int kOut, int kNT>
+hipError_t launch_few_rows(const FewArgs &g, hipStream_t s) {
+  if (g.m >= 64 * 512) return launch_few<D, kXFormat, kWFormat, kOut, kNT <= 2 ? 4 : 2, kNT>(g, s);
+  if (g.m >= 32 * 512) return launch_few<D, kXFormat, kWFormat, kOut, 2, kNT>(g, s);
+  return launch_few<D, kXFormat, kWFormat, kOut, 1, kNT>(g, s);
+}
+
+unsigned grid_of(int64_t blocks) { return (unsigned)(blocks < (1 << 20) ? blocks : 1 << 20); }
+
+constexpr int64_t kFewDense = 16, kFewTokens = 64;
+
 }  // namespace
 
 hipError_t launch_fp8_quantize(const void *src, int dtype, int64_t rows, int64_t cols, int format,
                                uint8_t *codes, uint8_t *scales, hipStream_t s) {
-  const unsigned tiles = (unsigned)(blocks_up(rows) * blocks_up(cols));
-  return with_dense(dtype, [&](auto t) {
+  const int64_t tiles = blocks_up(rows) * blocks_up(cols);
+  return with_type(dtype, [&](auto d) {
+    using D = decltype(d);
     return with_format(format, [&](auto f) {
-      quantize_kernel<t.value, f.value><<<tiles, 256, 0, s>>>(src, rows, cols, codes, scales);
+      quantize_kernel<D, f.value><<<grid_of(tiles), 256, 0, s>>>(
+          static_cast<const typename D::raw *>(src), rows, cols, codes, scales, tiles);
       return hipGetLastError();
     });
   });
 }
 
 hipError_t launch_fp8_dequantize(const af1_fp8_matrix &W, void *dst, int dtype, hipStream_t s) {
-  const unsigned tiles = (unsigned)(blocks_up(W.rows) * blocks_up(W.cols));
-  return with_dense(dtype, [&](auto t) {
+  const int64_t tiles = blocks_up(W.rows) * blocks_up(W.cols);
+  return with_type(dtype, [&](auto d) {
+    using D = decltype(d);
     return with_format(W.format, [&](auto f) {
-      dequantize_kernel<t.value, f.value>
-          <<<tiles, 256, 0, s>>>(W.codes, W.scales, W.rows, W.cols, dst);
+      dequantize_kernel<D, f.value><<<grid_of(tiles), 256, 0, s>>>(
+          W.codes, W.scales, W.rows, W.cols, static_cast<typename D::raw *>(dst), tiles);
       return hipGetLastError();
     });
   });
@@ -607,32 +808,49 @@ hipError_t launch_fp8_dequantize(const af1_fp8_matrix &W, void *dst, int dtype, 
 hipError_t launch_fp8_transpose(const af1_fp8_matrix &W, uint8_t *codes, uint8_t *scales,
                                 hipStream_t s) {
   const int64_t R = blocks_up(W.rows), C = blocks_up(W.cols);
-  transpose_tiles_kernel<<<(unsigned)(R * C), 256, 0, s>>>(W.codes, W.scales, R, C, codes, scales);
+  transpose_tiles_kernel<<<grid_of(R * C), 256, 0, s>>>(W.codes, W.scales, R, C, codes, scales);
   return hipGetLastError();
 }
 
 size_t fp8_linear_workspace_bytes(int64_t, int64_t n, int64_t T) {
+  if (T <= kFewDense) return 0;
   return (size_t)blocks_up(T) * blocks_up(n) * (kTileBytes + kBlk);
+}
+
+template <int kXFormat, int kWFormat, int kOut>
+hipError_t launch_linear(const af1_fp8_matrix &W, const void *x, int x_dtype, int64_t T, void *y,
+                         void *ws, hipStream_t s) {
+  const int64_t m = W.rows, n = W.cols;
+  const XTiles xt = x_tiles(ws, n, T);
+  FewArgs few{W.codes, W.scales, x, xt, (int)T, m, n, y};
+  if (T <= kFewDense)
+    return with_type(x_dtype, [&](auto d) {
+      return launch_few_rows<decltype(d), kXFormat, kWFormat, kOut, 1>(few, s);
+    });
+  const hipError_t e = with_type(x_dtype, [&](auto d) {
+    using D = decltype(d);
+    quantize_rows_kernel<D, kXFormat><<<grid_of((T * blocks_up(n) + 15) / 16), 256, 0, s>>>(
+        static_cast<const typename D::raw *>(x), T, n, xt);
+    return hipGetLastError();
+  });
+  if (e != hipSuccess) return e;
+  if (T <= 32) return launch_few_rows<F32, kXFormat, kWFormat, kOut, 2>(few, s);
+  if (T <= kFewTokens) return launch_few_rows<F32, kXFormat, kWFormat, kOut, 4>(few, s);
+  LinearArgs g{W.codes, W.scales, xt, T, m, (int)blocks_up(n), (int)blocks_up(m),
+               (int)blocks_up(T), 0, 0, y};
+  if (kOut == AF1_SRC_F32 || T <= 1024)
+    return launch_tiles<Tile<128, 128, 2, 2, 4>, kWFormat, kXFormat, kOut>(g, s);
+  if constexpr (kOut == AF1_SRC_BF16)
+    return launch_tiles<Tile<256, 256, 2, 2, 4>, kWFormat, kXFormat, kOut>(g, s);
 }
 
 hipError_t launch_fp8_linear(const af1_fp8_matrix &W, const void *x, int x_dtype, int x_format,
                              int64_t T, void *y, int y_dtype, void *ws, hipStream_t s) {
-  const int64_t m = W.rows, n = W.cols;
-  const XTiles xt = x_tiles(ws, n, T);
   return with_format(x_format, [&](auto xf) {
-    const hipError_t e = with_dense(x_dtype, [&](auto t) {
-      quantize_rows_kernel<t.value, xf.value>
-          <<<(unsigned)((T * blocks_up(n) + 15) / 16), 256, 0, s>>>(x, T, n, xt);
-      return hipGetLastError();
-    });
-    if (e != hipSuccess) return e;
     return with_format(W.format, [&](auto wf) {
-      LinearArgs g{W.codes, W.scales, xt, T, m, (int)blocks_up(n), (int)blocks_up(m),
-                   (int)blocks_up(T), 0, 0, y};
       if (y_dtype == AF1_SRC_F32)
-        return launch_tiles<Tile<128, 128, 2, 2, 4>, wf.value, xf.value, AF1_SRC_F32>(g, s);
-      if (T <= 1024) return launch_tiles<Tile<128, 128, 2, 2, 4>, wf.value, xf.value, AF1_SRC_BF16>(g, s);
-      return launch_tiles<Tile<256, 256, 2, 2, 4>, wf.value, xf.value, AF1_SRC_BF16>(g, s);
+        return launch_linear<xf.value, wf.value, AF1_SRC_F32>(W, x, x_dtype, T, y, ws, s);
+      return launch_linear<xf.value, wf.value, AF1_SRC_BF16>(W, x, x_dtype, T, y, ws, s);
     });
   });
 }

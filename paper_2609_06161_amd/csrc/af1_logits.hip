@@ -17,7 +17,7 @@
 // are few, whose statistics a second launch joins in the parts' order.
 #include <math.h>
 
-#include "af1_device.h"
+#include "af1_head_device.h"
 #include "af1_head_internal.h"
 
 // Products and sums are fused only where it is written: a student equal to its
@@ -27,75 +27,9 @@
 namespace af1h {
 namespace {
 
-using af1::bf16_to_f32;
-using af1::f16_to_f32;
-using af1::f32_to_bf16;
-using af1::f32_to_f16;
-
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_inff();
-
-// Element types of logits.
-struct F32 {
-  using raw = float;
-  static __device__ __forceinline__ float get(float v) { return v; }
-  static __device__ __forceinline__ float put(float v) { return v; }
-};
-struct BF16 {
-  using raw = uint16_t;
-  static __device__ __forceinline__ float get(uint16_t v) { return bf16_to_f32(v); }
-  static __device__ __forceinline__ uint16_t put(float v) { return f32_to_bf16(v); }
-};
-struct F16 {
-  using raw = uint16_t;
-  static __device__ __forceinline__ float get(uint16_t v) { return f16_to_f32(v); }
-  static __device__ __forceinline__ uint16_t put(float v) { return f32_to_f16(v); }
-};
-
-// Eight elements, aligned as one: rows of odd length or stride start anywhere.
-template <typename R>
-struct __attribute__((packed, aligned(sizeof(R)))) Eight {
-  R v[8];
-};
-
-template <typename D>
-__device__ __forceinline__ Eight<typename D::raw> load_raw(const typename D::raw *row, int64_t c) {
-  return *reinterpret_cast<const Eight<typename D::raw> *>(row + 8 * c);
-}
-
-template <typename D>
-__device__ __forceinline__ void widen(const Eight<typename D::raw> &e, float (&x)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = D::get(e.v[i]);
-}
-
-// Elements 8 c .. 8 c + 7 of a row of V; -infinity stands behind the end.
-template <typename D>
-__device__ __forceinline__ void load8(const typename D::raw *row, int64_t c, int64_t V,
-                                      float (&x)[8]) {
-  if (8 * c + 8 <= V) {
-    widen<D>(load_raw<D>(row, c), x);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = 8 * c + i < V ? D::get(row[8 * c + i]) : -kInf;
-  }
-}
-
-template <typename D>
-__device__ __forceinline__ void store8(typename D::raw *row, int64_t c, int64_t V,
-                                       const float (&x)[8]) {
-  if (8 * c + 8 <= V) {
-    Eight<typename D::raw> e;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) e.v[i] = D::put(x[i]);
-    *reinterpret_cast<Eight<typename D::raw> *>(row + 8 * c) = e;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (8 * c + i < V) row[8 * c + i] = D::put(x[i]);
-  }
-}
 
 __device__ __forceinline__ float exp2_hw(float t) { return __builtin_amdgcn_exp2f(t); }
 
@@ -240,7 +174,7 @@ __device__ __forceinline__ void each_chunk(const typename D::raw *row, int64_t c
   }
   for (; i < c1; i += kThreads) {
     float x[8];
-    load8<D>(row, i, V, x);
+    load8<D>(row, i, V, -kInf, x);
     f(i, x);
   }
 }
@@ -361,7 +295,7 @@ __device__ uint64_t part_top(const typename D::raw *row, int64_t c0, int64_t c1,
     const int64_t c = c0 + l.holders[i / each] + i % each * kThreads;
     if (c >= c1) continue;
     float x[8];
-    load8<D>(row, c, V, x);
+    load8<D>(row, c, V, -kInf, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (8 * c + e < V) collect(l, order_key(x[e], 8 * c + e));
@@ -567,8 +501,8 @@ __device__ __forceinline__ void each_pair(const typename D::raw *s, const typena
   }
   for (; i < c1; i += kThreads) {
     float x[8], w[8];
-    load8<D>(s, i, V, x);
-    load8<D>(t, i, V, w);
+    load8<D>(s, i, V, -kInf, x);
+    load8<D>(t, i, V, -kInf, w);
     f(i, x, w);
   }
 }
@@ -689,13 +623,6 @@ __global__ __launch_bounds__(kThreads) void kl_sum_kernel(int64_t T, KlArgs g) {
   for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
   const KlRow k = kl_join(r, T, g);
   if (lane == 0) g.kl[r] = k.none ? k.instead : sum;
-}
-
-template <typename F>
-auto with_type(int dtype, F &&f) {
-  if (dtype == AF1_SRC_F32) return f(F32{});
-  if (dtype == AF1_SRC_BF16) return f(BF16{});
-  return f(F16{});
 }
 
 // Parts of a row for T rows: as many as give the device kWant blocks, of at

@@ -85,7 +85,7 @@ def test_dequantize_and_transpose_refusals():
     assert tr(codes=P[0]) == ALIAS and tr(scales=P[3]) == ALIAS and tr(scales=P[1]) == ALIAS
 
 
-def linear(W=matrix(), x=P[2], xd=af1.AF1_SRC_BF16, xf=0, T=5, y=P[3], yd=af1.AF1_SRC_F32,
+def linear(W=matrix(), x=P[2], xd=af1.AF1_SRC_BF16, xf=0, T=70, y=P[3], yd=af1.AF1_SRC_F32,
            ws=P[4], ws_bytes=BIG):
     return head.af1_fp8_linear(W, x, xd, xf, T, y, yd, ws, ws_bytes, stream=0, check=False)
 
@@ -100,7 +100,7 @@ def test_linear_refusals():
     assert linear(matrix(codes=None)) == NULL
     for k in ("x", "y", "ws"):
         assert linear(**{k: P[5] + 2}) == ALIGN
-    need = head.af1_fp8_linear_workspace_bytes(256, 300, 5)
+    need = head.af1_fp8_linear_workspace_bytes(256, 300, 70)
     assert linear(ws=None) == WS and linear(ws_bytes=need - 1) == WS
     for y in (P[0], P[1], P[2], P[4]):
         assert linear(y=y) == ALIAS
