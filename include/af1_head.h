@@ -182,12 +182,13 @@ AF1_API af1_status af1_token_logprobs_backward(const void *logits, int32_t dtype
  *              loss alone.  It may be the student's own array where ldd = ld_s,
  *              and must not overlap any array otherwise.
  *   ws       : device, af1_distill_kl_workspace_bytes(T, V) bytes.
- * kl is summed as p_j (exp(-u) - 1 + u), u = log p_j - log q_j: no term is
- * negative, so a small divergence keeps its digits.  An entry whose p_j
- * underflows adds q_j only.  Where the student masks (-infinity) an entry of
- * the teacher's, kl is infinite.  A token whose teacher masks everything has
- * kl 0; its gradient is zero, and so are those of tokens of weight 0 and of
- * tokens whose student masks everything.  NaN or +infinity in a row gives NaN.
+ * kl is summed from the differences of the two logits, not of two logarithms,
+ * so a small divergence keeps its digits; none is below 0.
+ * Entries whose p_j is 0 in fp32 add nothing.  Where the student masks
+ * (-infinity) an entry of the teacher's, kl is infinite.  A token whose teacher
+ * masks everything has kl 0; its gradient is zero, and so are those of tokens
+ * of weight 0 and of tokens whose student masks everything.  NaN or +infinity
+ * in a row gives NaN.
  */
 AF1_API size_t af1_distill_kl_workspace_bytes(int64_t T, int64_t V);
 AF1_API af1_status af1_distill_kl(const void *student, const void *teacher, int32_t dtype,

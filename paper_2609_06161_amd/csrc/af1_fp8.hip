@@ -596,7 +596,7 @@ __device__ __forceinline__ v8i operand(const RowCodes &c) {
 
 template <typename D>
 struct DenseRow {
-  Eight<typename D::raw> v[4];
+  Eight<D> v[4];
 };
 
 template <typename D, int kXFormat, int kWFormat, int kOut, int kFR, int kNT, int kWaves>
@@ -632,13 +632,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs g) {
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         const int at = (c & 1) * 8 + (c >> 1) * 64;
-        if (r < g.T && at + 8 <= left) {
-          b.d.v[c] = *reinterpret_cast<const Eight<typename D::raw> *>(p + at);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            b.d.v[c].v[i] = r < g.T && at + i < left ? p[at + i] : (typename D::raw)0;
-        }
+        b.d.v[c] = load_raw_to<D>(p + at, 0, r < g.T ? left - at : 0, 0.f);
       }
     } else {
 #pragma unroll
@@ -737,6 +731,152 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs g) {
   }
 }
 
+// ---------------------------------------------------------------------------
+// Up to 16 tokens.  x rounded to 8 bits stays in LDS as operands, two KiB a
+// column block, and each wave streams strips of 16 rows of W past it.  A ring
+// of kRing blocks is in flight a wave, across the ends of strips: memory sees
+// one unbroken stream.  When there are fewer strips than waves, kSplit waves
+// share a strip, every kSplit-th block each, and add their sums in LDS in
+// order.
+// ---------------------------------------------------------------------------
+
+constexpr int kStripWaves = 8;
+
+template <typename D, int kXFormat, int kWFormat, int kOut, int kSplit>
+__global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(FewArgs g) {
+  constexpr int kRing = 8, kStrips = kStripWaves / kSplit;  // strips at a time
+  extern __shared__ uint8_t lds[];  // operands [C][2][64][16], scales [C][16], sums
+  const int64_t n = g.n;
+  const int C = (int)((n + kBlk - 1) / kBlk);
+  uint8_t *xs = lds + C * 2048;
+  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int part = wave % kSplit;
+
+  // this wave's strips: strip0, strip0 + stride, ...; each of its blocks
+  // part, part + kSplit, ...
+  const int strips = (int)((g.m + 15) / 16), stride = (int)gridDim.x * kStrips;
+  const int strip0 = (int)blockIdx.x * kStrips + wave / kSplit;
+  const int each = (C - part + kSplit - 1) / kSplit;
+  const int rounds = strip0 < strips ? (strips - strip0 + stride - 1) / stride : 0;
+  const int total = rounds * each;
+
+  // the ring's next block
+  int ls = strip0, lj = 0;
+  struct Block {
+    i32x4 lo, hi;
+    int sw;
+  } ring[kRing];
+  auto load = [&](Block &b) {
+    const int64_t row = (int64_t)ls * 16;
+    const int J = part + lj * kSplit;
+    const int64_t tile = row / kBlk * C + J;
+    const i32x4 *p = reinterpret_cast<const i32x4 *>(g.wcodes + tile * kTileBytes +
+                                                     (row % kBlk + r) * kBlk + q * 16);
+    b.lo = p[0];
+    b.hi = p[4];
+    b.sw = g.wscales[tile];
+    if (++lj == each) lj = 0, ls += stride;
+  };
+#pragma unroll
+  for (int u = 0; u < kRing; ++u)
+    if (u < total) load(ring[u]);
+
+  // x, sixteen lanes a token and block
+  {
+    const typename D::raw *x = static_cast<const typename D::raw *>(g.x);
+    const int k = threadIdx.x & 15;
+    for (int piece = threadIdx.x >> 4; piece < g.T * C; piece += 4 * kStripWaves) {
+      const int t = piece / C, J = piece % C;
+      float v[8], amax = 0.f;
+      load8<D>(x + t * n + (int64_t)J * kBlk, k, n - (int64_t)J * kBlk, 0.f, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_abs(v[i]));
+#pragma unroll
+      for (int off = 8; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 16));
+      const int e = block_exponent<kXFormat>(amax);
+      // columns 8 k .. belong to half k / 8, lane group (k / 2) mod 4
+      *reinterpret_cast<uint2 *>(lds + J * 2048 + (k >> 3) * 1024 + ((k >> 1 & 3) * 16 + t) * 16 +
+                                 (k & 1) * 8) = encode8<kXFormat>(v, pow2(-e));
+      if (k == 0) xs[J * 16 + t] = (uint8_t)(e + 127);
+    }
+  }
+  __syncthreads();
+
+  v4f acc = {};
+  auto multiply = [&](const Block &b, int J) {
+    // entries of tokens behind T are whatever LDS held; they stay in columns
+    // that are not stored
+    const uint8_t *p = lds + J * 2048 + lane * 16;
+    const RowCodes x{*reinterpret_cast<const i32x4 *>(p), *reinterpret_cast<const i32x4 *>(p + 1024)};
+    const int sx = xs[J * 16 + r];
+    const v8i w = operand(RowCodes{b.lo, b.hi});
+    if constexpr (kOut == AF1_SRC_BF16) {
+      acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, operand(x), acc, kWFormat, kXFormat,
+                                                             0, b.sw, 0, sx);
+    } else {
+      bf8v a[4], c[4];
+      to_bf16<kWFormat>(w, a);
+      to_bf16<kXFormat>(operand(x), c);
+      v4f s = {};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[k], c[k], s, 0, 0, 0);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc[k] += ldexpf(s[k], b.sw + sx - 254);
+    }
+  };
+  auto store = [&](int strip, v4f v) {
+    const int64_t row = (int64_t)strip * 16 + 4 * q;
+    if (r >= g.T) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (row + i < g.m) {
+        const int64_t at = (int64_t)r * g.m + row + i;
+        if constexpr (kOut == AF1_SRC_F32)
+          static_cast<float *>(g.y)[at] = v[i];
+        else
+          static_cast<uint16_t *>(g.y)[at] = f32_to_bf16(v[i]);
+      }
+  };
+
+  if constexpr (kSplit == 1) {
+    int strip = strip0, j = 0;
+    for (int i = 0; i < total; i += kRing) {
+#pragma unroll
+      for (int u = 0; u < kRing; ++u) {
+        if (i + u < total) {
+          multiply(ring[u], j);
+          if (++j == each) {
+            store(strip, acc);
+            acc = v4f{};
+            j = 0;
+            strip += stride;
+          }
+        }
+        if (i + u + kRing < total) load(ring[u]);
+      }
+    }
+  } else {
+    // one round: the launch has a workgroup for every kStrips strips
+    v4f *sums = reinterpret_cast<v4f *>(lds + ((C * 2064 + 15) & ~15));
+    for (int i = 0; i < total; i += kRing) {
+#pragma unroll
+      for (int u = 0; u < kRing; ++u) {
+        if (i + u < total) multiply(ring[u], part + (i + u) * kSplit);
+        if (i + u + kRing < total) load(ring[u]);
+      }
+    }
+    sums[wave * 64 + lane] = acc;
+    __syncthreads();
+    if (part == 0 && strip0 < strips) {
+      v4f s = acc;
+#pragma unroll
+      for (int k = 1; k < kSplit; ++k) s += sums[(wave + k) * 64 + lane];
+      store(strip0, s);
+    }
+  }
+}
+
 template <int kV>
 struct Int {
   static constexpr int value = kV;
@@ -774,8 +914,28 @@ hipError_t launch_few_rows(const FewArgs &g, hipStream_t s) {
   return launch_few<D, kXFormat, kWFormat, kOut, 1, kNT>(g, s);
 }
 
+template <typename D, int kXFormat, int kWFormat, int kOut, int kSplit>
+hipError_t launch_strips(const FewArgs &g, hipStream_t s) {
+  const int64_t C = blocks_up(g.n), groups = (g.m + 16 * (kStripWaves / kSplit) - 1) / (16 * (kStripWaves / kSplit));
+  const size_t lds = ((C * 2064 + 15) & ~15) + (kSplit > 1 ? kStripWaves * 1024 : 0);
+  const int64_t resident = device_cus() * (lds <= 80 * 1024 ? 2 : 1);
+  const int64_t blocks = kSplit > 1 || groups < resident ? groups : resident;
+  strip_kernel<D, kXFormat, kWFormat, kOut, kSplit><<<(unsigned)blocks, 64 * kStripWaves, lds, s>>>(g);
+  return hipGetLastError();
+}
+
+template <typename D, int kXFormat, int kWFormat, int kOut>
+hipError_t launch_strip_form(const FewArgs &g, hipStream_t s) {
+  const int64_t strips = (g.m + 15) / 16, cus = device_cus();
+  if (strips >= 8 * cus) return launch_strips<D, kXFormat, kWFormat, kOut, 1>(g, s);
+  if (strips >= 4 * cus) return launch_strips<D, kXFormat, kWFormat, kOut, 2>(g, s);
+  if (strips >= 2 * cus) return launch_strips<D, kXFormat, kWFormat, kOut, 4>(g, s);
+  return launch_strips<D, kXFormat, kWFormat, kOut, 8>(g, s);
+}
+
 unsigned grid_of(int64_t blocks) { return (unsigned)(blocks < (1 << 20) ? blocks : 1 << 20); }
 
+constexpr int64_t kStripBlocks = 72;  // as many as LDS holds
 constexpr int64_t kFewDense = 16, kFewTokens = 64;
 
 }  // namespace
@@ -823,6 +983,10 @@ hipError_t launch_linear(const af1_fp8_matrix &W, const void *x, int x_dtype, in
   const int64_t m = W.rows, n = W.cols;
   const XTiles xt = x_tiles(ws, n, T);
   FewArgs few{W.codes, W.scales, x, xt, (int)T, m, n, y};
+  if (T <= kFewDense && blocks_up(n) <= kStripBlocks)
+    return with_type(x_dtype, [&](auto d) {
+      return launch_strip_form<decltype(d), kXFormat, kWFormat, kOut>(few, s);
+    });
   if (T <= kFewDense)
     return with_type(x_dtype, [&](auto d) {
       return launch_few_rows<decltype(d), kXFormat, kWFormat, kOut, 1>(few, s);

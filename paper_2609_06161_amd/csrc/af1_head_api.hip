@@ -4,9 +4,28 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "af1_check.h"
 #include "af1_head.h"
 #include "af1_head_internal.h"
+
+namespace af1h {
+
+int device_cus() {
+  static std::atomic<int> cache[64];
+  int dev = 0, cus = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+  cus = cache[dev].load(std::memory_order_relaxed);
+  if (cus > 0) return cus;
+  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
+      cus <= 0)
+    return 256;
+  cache[dev].store(cus, std::memory_order_relaxed);
+  return cus;
+}
+
+}  // namespace af1h
 
 using namespace af1::check;
 using af1h::blocks_up;

@@ -30,43 +30,73 @@ auto with_type(int dtype, F &&f) {
   return f(F16{});
 }
 
-// Eight elements, aligned as one: rows of odd length or stride start anywhere.
-template <typename R>
-struct __attribute__((packed, aligned(sizeof(R)))) Eight {
-  R v[8];
+// Eight elements as they are stored, aligned as one: rows of odd length or
+// stride start anywhere.  16-bit elements stay packed in four registers.
+template <typename D>
+struct __attribute__((packed, aligned(sizeof(typename D::raw)))) Eight {
+  uint32_t w[2 * sizeof(typename D::raw)];
 };
 
 template <typename D>
-__device__ __forceinline__ Eight<typename D::raw> load_raw(const typename D::raw *row, int64_t c) {
-  return *reinterpret_cast<const Eight<typename D::raw> *>(row + 8 * c);
+__device__ __forceinline__ Eight<D> load_raw(const typename D::raw *row, int64_t c) {
+  return *reinterpret_cast<const Eight<D> *>(row + 8 * c);
+}
+
+// The elements i of 0 .. 7 for which in(i), others `fill`.
+template <typename D, typename F>
+__device__ __forceinline__ Eight<D> load_some(const typename D::raw *p, F &&in, float fill) {
+  Eight<D> e;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(e) / 4); ++i) {
+    if constexpr (sizeof(typename D::raw) == 4) {
+      e.w[i] = __float_as_uint(in(i) ? p[i] : fill);
+    } else {
+      const uint32_t lo = in(2 * i) ? p[2 * i] : D::put(fill);
+      const uint32_t hi = in(2 * i + 1) ? p[2 * i + 1] : D::put(fill);
+      e.w[i] = lo | hi << 16;
+    }
+  }
+  return e;
 }
 
 template <typename D>
-__device__ __forceinline__ void widen(const Eight<typename D::raw> &e, float (&x)[8]) {
+__device__ __forceinline__ void widen(const Eight<D> &e, float (&x)[8]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = D::get(e.v[i]);
+  for (int i = 0; i < 8; ++i) {
+    if constexpr (sizeof(typename D::raw) == 4)
+      x[i] = __uint_as_float(e.w[i]);
+    else
+      x[i] = D::get((uint16_t)(e.w[i >> 1] >> (16 * (i & 1))));
+  }
 }
 
 // Elements 8 c .. 8 c + 7 of a row of V; `fill` stands behind the end.
 template <typename D>
+__device__ __forceinline__ Eight<D> load_raw_to(const typename D::raw *row, int64_t c, int64_t V,
+                                                float fill) {
+  if (8 * c + 8 <= V) return load_raw<D>(row, c);
+  return load_some<D>(row + 8 * c, [&](int i) { return 8 * c + i < V; }, fill);
+}
+
+template <typename D>
 __device__ __forceinline__ void load8(const typename D::raw *row, int64_t c, int64_t V, float fill,
                                       float (&x)[8]) {
-  if (8 * c + 8 <= V) {
-    widen<D>(load_raw<D>(row, c), x);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = 8 * c + i < V ? D::get(row[8 * c + i]) : fill;
-  }
+  widen<D>(load_raw_to<D>(row, c, V, fill), x);
 }
 
 template <typename D>
 __device__ __forceinline__ void store8(typename D::raw *row, int64_t c, int64_t V,
                                        const float (&x)[8]) {
   if (8 * c + 8 <= V) {
-    Eight<typename D::raw> e;
+    Eight<D> e;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e.v[i] = D::put(x[i]);
-    *reinterpret_cast<Eight<typename D::raw> *>(row + 8 * c) = e;
+    for (int i = 0; i < (int)(sizeof(e) / 4); ++i) {
+      if constexpr (sizeof(typename D::raw) == 4)
+        e.w[i] = __float_as_uint(x[i]);
+      else
+        e.w[i] = (uint32_t)D::put(x[2 * i]) | (uint32_t)D::put(x[2 * i + 1]) << 16;
+    }
+    *reinterpret_cast<Eight<D> *>(row + 8 * c) = e;
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)

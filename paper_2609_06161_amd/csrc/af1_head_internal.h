@@ -11,6 +11,10 @@ namespace af1h {
 
 constexpr int kBlk = 128;  // rows and columns of a block that share a scale
 
+// Compute units of the current device (queried once per device; 256 if the
+// query fails).
+int device_cus();
+
 inline int64_t blocks_up(int64_t n) { return (n + kBlk - 1) / kBlk; }
 
 hipError_t launch_fp8_quantize(const void *src, int dtype, int64_t rows, int64_t cols, int format,

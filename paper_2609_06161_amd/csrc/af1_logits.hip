@@ -12,9 +12,9 @@
 // is taken before the product with c, so that a row of the type's lowest
 // values (a mask that is no infinity) neither overflows nor cancels.
 //
-// Work is cut into parts of a row (plan_parts): whole rows when there are
-// enough of them to fill the device, parts of at least 2048 logits when there
-// are few, whose statistics a second launch joins in the parts' order.
+// Work is cut into parts of a row: whole rows when there are enough of them to
+// fill the device, parts of at least 2048 logits when there are few.  Parts'
+// results are joined in the parts' order.
 #include <math.h>
 
 #include "af1_head_device.h"
@@ -33,69 +33,106 @@ constexpr float kInf = __builtin_inff();
 
 __device__ __forceinline__ float exp2_hw(float t) { return __builtin_amdgcn_exp2f(t); }
 
-// Running softmax statistics.  NaN logits leave m alone and make Z NaN, and so
-// does +infinity (infinity less itself).
+// One value a lane combined over the 64 lanes in a fixed order, in every lane:
+// four DPP steps within rows of 16, then the four rows.
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kCtrl, 0xF, 0xF, false));
+}
+template <typename Op>
+__device__ __forceinline__ float wave_all(float v, Op op) {
+  v = op(v, dpp<0xB1>(v));   // lane ^ 1
+  v = op(v, dpp<0x4E>(v));   // lane ^ 2
+  v = op(v, dpp<0x124>(v));  // row rotated by 4
+  v = op(v, dpp<0x128>(v));  // and by 8
+  const int i = __float_as_int(v);
+  const float r0 = __int_as_float(__builtin_amdgcn_readlane(i, 0));
+  const float r1 = __int_as_float(__builtin_amdgcn_readlane(i, 16));
+  const float r2 = __int_as_float(__builtin_amdgcn_readlane(i, 32));
+  const float r3 = __int_as_float(__builtin_amdgcn_readlane(i, 48));
+  return op(op(r0, r1), op(r2, r3));
+}
+__device__ __forceinline__ float wave_add(float v) {
+  return wave_all(v, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float wave_max(float v) {
+  return wave_all(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
+__device__ __forceinline__ float max8(const float (&x)[8]) {
+  return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
+               fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+}
+
+// Running softmax statistics (W where kEntropy).  NaN logits leave m alone and
+// make Z NaN, and so does +infinity (infinity less itself).
 struct Stat {
   float m, Z, W;
 };
 __device__ __forceinline__ Stat no_logits() { return Stat{-kInf, 0.f, 0.f}; }
 
-template <int kN>
-__device__ __forceinline__ void add(Stat &s, const float (&x)[kN], float c) {
-  float m = s.m;
-#pragma unroll
-  for (int i = 0; i < kN; ++i) m = fmaxf(m, x[i]);
+// The statistics about `m`, at least s.m.
+template <bool kEntropy>
+__device__ __forceinline__ void rebase(Stat &s, float m, float c) {
   // nothing but masked entries so far: any finite base gives them 2^-inf = 0
-  const float base = m == -kInf ? 0.f : m;
-  const float step = s.m == -kInf ? 0.f : (s.m - base) * c;
+  const float step = s.m == -kInf ? 0.f : (s.m - m) * c;
   const float f = exp2_hw(step);
   // a step of -infinity empties both sums
-  s.W = f == 0.f ? 0.f : f * fmaf(step, s.Z, s.W);
+  if constexpr (kEntropy) s.W = f == 0.f ? 0.f : f * fmaf(step, s.Z, s.W);
   s.Z *= f;
   s.m = m;
+}
+
+// Eight logits, the largest of which is `top`.
+template <bool kEntropy>
+__device__ __forceinline__ void add8(Stat &s, const float (&x)[8], float top, float c) {
+  rebase<kEntropy>(s, fmaxf(s.m, top), c);
+  const float base = s.m == -kInf ? 0.f : s.m;
 #pragma unroll
-  for (int i = 0; i < kN; ++i) {
+  for (int i = 0; i < 8; ++i) {
     const float t = (x[i] - base) * c;
     const float e = exp2_hw(t);
     s.Z += e;
-    s.W = fmaf(e, fmaxf(t, -200.f), s.W);  // 2^-200 is 0 in fp32: masked entries add 0
+    // 2^-200 is 0 in fp32: masked entries add 0
+    if constexpr (kEntropy) s.W = fmaf(e, fmaxf(t, -200.f), s.W);
   }
 }
 
-__device__ __forceinline__ Stat join(Stat a, Stat b, float c) {
-  Stat r;
-  r.m = fmaxf(a.m, b.m);
-  const float base = r.m == -kInf ? 0.f : r.m;
-  const float sa = a.m == -kInf ? 0.f : (a.m - base) * c, fa = exp2_hw(sa);
-  const float sb = b.m == -kInf ? 0.f : (b.m - base) * c, fb = exp2_hw(sb);
-  r.Z = fmaf(a.Z, fa, b.Z * fb);
-  r.W = (fa == 0.f ? 0.f : fa * fmaf(sa, a.Z, a.W)) + (fb == 0.f ? 0.f : fb * fmaf(sb, b.Z, b.W));
-  return r;
-}
-
+template <bool kEntropy>
 __device__ __forceinline__ Stat wave_join(Stat s, float c) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    Stat o;
-    o.m = __shfl_xor(s.m, off, 64);
-    o.Z = __shfl_xor(s.Z, off, 64);
-    o.W = __shfl_xor(s.W, off, 64);
-    s = join(s, o, c);
-  }
+  rebase<kEntropy>(s, wave_max(s.m), c);
+  s.Z = wave_add(s.Z);
+  if constexpr (kEntropy) s.W = wave_add(s.W);
   return s;
 }
 
+// The statistics (without entropy) of two sets of logits together.
+__device__ __forceinline__ Stat join2(Stat a, Stat b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  rebase<false>(a, m, c);
+  rebase<false>(b, m, c);
+  return Stat{m, a.Z + b.Z, 0.f};
+}
+
+constexpr int kThreads = 256;  // of every kernel here
+constexpr int kWaves = kThreads / 64;
+
 // The block's statistics, in every thread; sh holds one entry a wave.
-template <int kN>
+template <bool kEntropy>
 __device__ __forceinline__ Stat block_join(Stat s, float c, Stat *sh) {
-  s = wave_join(s, c);
-  if constexpr (kN > 64) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
-    __syncthreads();
-    s = sh[0];
+  s = wave_join<kEntropy>(s, c);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+  __syncthreads();
+  Stat w[kWaves];
+  float m = -kInf;
 #pragma unroll
-    for (int w = 1; w < kN / 64; ++w) s = join(s, sh[w], c);
+  for (int i = 0; i < kWaves; ++i) w[i] = sh[i], m = fmaxf(m, w[i].m);
+  s = Stat{m, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    rebase<kEntropy>(w[i], m, c);
+    s.Z += w[i].Z;
+    s.W += w[i].W;
   }
   return s;
 }
@@ -108,6 +145,11 @@ __device__ __forceinline__ uint64_t order_key(float x, int64_t index) {
   return (uint64_t)u << 32 | (uint32_t)~(uint32_t)index;
 }
 __device__ __forceinline__ uint32_t key_index(uint64_t key) { return ~(uint32_t)key; }
+
+template <int kV>
+struct Int {
+  static constexpr int value = kV;
+};
 
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
@@ -144,9 +186,6 @@ __device__ void write_row(const RowOut &o, const typename D::raw *row, int64_t r
   }
 }
 
-constexpr int kThreads = 256;  // of every kernel here
-constexpr int kWaves = kThreads / 64;
-
 // A row's parts: `size` chunks of eight logits each (the last may be short).
 struct Parts {
   int count;
@@ -162,7 +201,7 @@ __device__ __forceinline__ void each_chunk(const typename D::raw *row, int64_t c
   const int64_t whole = min(c1, V / 8);
   int64_t i = c0 + threadIdx.x;
   for (; i + (kAhead - 1) * kThreads < whole; i += kAhead * kThreads) {
-    Eight<typename D::raw> e[kAhead];
+    Eight<D> e[kAhead];
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) e[a] = load_raw<D>(row, i + a * kThreads);
 #pragma unroll
@@ -185,7 +224,9 @@ __device__ __forceinline__ void each_chunk(const typename D::raw *row, int64_t c
 // logit from below, and only the threads at or above it, at most k, can hold
 // one of the best: their chunks are read again (from the caches), what reaches
 // the bound is collected and sorted.  Keys are distinct, so equal logits need
-// no special case.
+// no special case.  Rows with NaN, which the threads' largest logits do not
+// see, and rows with more to collect than there is room for are searched once
+// for every alternative.
 // ---------------------------------------------------------------------------
 
 constexpr int kMaxFound = 512;  // collected logits; beyond it, one at a time
@@ -202,29 +243,55 @@ __device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int mask) {
   return (uint64_t)__shfl_xor((unsigned long long)v, mask, 64);
 }
 
-__device__ __forceinline__ uint64_t exchange(uint64_t v, int mask, bool larger) {
-  const uint64_t o = shfl_xor64(v, mask);
+// The value of lane ^ kMask, by register moves.
+template <int kMask>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
+  const auto move = [](uint32_t u, auto ctrl) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)u, decltype(ctrl)::value, 0xF, 0xF, false);
+  };
+  if constexpr (kMask == 1) return move(v, Int<0xB1>{});
+  if constexpr (kMask == 2) return move(v, Int<0x4E>{});
+  // the lanes of eight mirrored (^ 7), then of four (^ 3)
+  if constexpr (kMask == 4) return move(move(v, Int<0x141>{}), Int<0x1B>{});
+  if constexpr (kMask == 8) return move(v, Int<0x128>{});  // the row rotated by 8
+  if constexpr (kMask == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return threadIdx.x & 16 ? r[0] : r[1];
+  }
+  if constexpr (kMask == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return threadIdx.x & 32 ? r[0] : r[1];
+  }
+}
+
+template <int kMask>
+__device__ __forceinline__ uint64_t exchange(uint64_t v, bool larger) {
+  const uint64_t o = (uint64_t)lane_xor<kMask>((uint32_t)(v >> 32)) << 32 | lane_xor<kMask>((uint32_t)v);
   return (v > o) == larger ? v : o;
+}
+
+// The steps of a bitonic merge of runs of 2 kMask keys, descending where `down`.
+template <int kMask>
+__device__ __forceinline__ uint64_t merge_steps(uint64_t v, bool down) {
+  v = exchange<kMask>(v, ((threadIdx.x & kMask) == 0) == down);
+  if constexpr (kMask > 1) v = merge_steps<kMask / 2>(v, down);
+  return v;
 }
 
 // Keys of a wave, the largest in lane 0 (bitonic).
 __device__ __forceinline__ uint64_t sort64(uint64_t v) {
   const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int k = 2; k <= 64; k <<= 1)
-#pragma unroll
-    for (int j = k >> 1; j > 0; j >>= 1)
-      v = exchange(v, j, ((lane & j) == 0) == ((lane & k) == 0));
-  return v;
+  v = merge_steps<1>(v, (lane & 2) == 0);
+  v = merge_steps<2>(v, (lane & 4) == 0);
+  v = merge_steps<4>(v, (lane & 8) == 0);
+  v = merge_steps<8>(v, (lane & 16) == 0);
+  v = merge_steps<16>(v, (lane & 32) == 0);
+  return merge_steps<32>(v, true);
 }
 
 // The largest 64 of two sorted lists, sorted.
 __device__ __forceinline__ uint64_t merge64(uint64_t a, const uint64_t *b) {
-  const int lane = threadIdx.x & 63;
-  uint64_t v = max64(a, b[63 - lane]);
-#pragma unroll
-  for (int j = 32; j > 0; j >>= 1) v = exchange(v, j, (lane & j) == 0);
-  return v;
+  return merge_steps<32>(max64(a, b[63 - (threadIdx.x & 63)]), true);
 }
 
 // In wave 0, lane i gets the i-th largest (i < 64) of the block's keys; the
@@ -279,10 +346,10 @@ __device__ __forceinline__ uint64_t one_by_one(int k, TopLds &l, F &&next) {
 
 // In wave 0, lane i gets the i-th largest key of the chunks c0 .. c1 - 1 (i <
 // k).  best, chunk: this thread's largest logit and the first chunk with it
-// (chunk < 0: the thread has none).
+// (chunk < 0: the thread has none).  odd: there may be NaN.
 template <typename D>
 __device__ uint64_t part_top(const typename D::raw *row, int64_t c0, int64_t c1, int64_t V, int k,
-                             float best, int64_t chunk, TopLds &l) {
+                             float best, int64_t chunk, bool odd, TopLds &l) {
   const uint64_t mine = chunk < 0 ? 0 : order_key(best, 8 * chunk + 7);
   uint64_t v = block_sort(mine, l);
   if (threadIdx.x == (unsigned)(k - 1)) l.bound = v;
@@ -301,7 +368,7 @@ __device__ uint64_t part_top(const typename D::raw *row, int64_t c0, int64_t c1,
       if (8 * c + e < V) collect(l, order_key(x[e], 8 * c + e));
   }
   __syncthreads();
-  if (l.n_found > kMaxFound)
+  if (odd || l.n_found > kMaxFound)
     return one_by_one(k, l, [&](uint64_t after) {
       uint64_t b = 0;
       for (int64_t i = 8 * c0 + threadIdx.x; i < min(8 * c1, V); i += kThreads) {
@@ -343,20 +410,14 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const typename D::ra
   float best = -kInf;
   int64_t chunk = -1;
   each_chunk<D>(row, c0, c1, V, [&](int64_t i, const float(&x)[8]) {
-    if constexpr (kTop) {
-      float m = x[0];
-      bool nan = x[0] != x[0];
-#pragma unroll
-      for (int e = 1; e < 8; ++e) m = fmaxf(m, x[e]), nan |= x[e] != x[e];
-      if (nan) m = __builtin_nanf("");
-      // NaN comes first
-      if (chunk < 0 || m > best || (m != m && best == best)) best = m, chunk = i;
-    }
-    add(s, x, c);
+    const float m = max8(x);
+    if constexpr (kTop)
+      if (chunk < 0 || m > best) best = m, chunk = i;
+    add8<true>(s, x, m, c);
   });
-  s = block_join<kThreads>(s, c, sh);
+  s = block_join<true>(s, c, sh);
   uint64_t key = 0;
-  if constexpr (kTop) key = part_top<D>(row, c0, c1, V, o.k, best, chunk, top);
+  if constexpr (kTop) key = part_top<D>(row, c0, c1, V, o.k, best, chunk, s.Z != s.Z, top);
   if (parts.count == 1) {
     if (threadIdx.x == 0) write_row<D>(o, row, r, V, s);
     if constexpr (kTop) write_top<D>(o, row, r, s, key);
@@ -368,9 +429,10 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const typename D::ra
 
 // Statistics of a row's parts (at most 64), joined in a fixed order; called by
 // a whole wave.
+template <bool kEntropy>
 __device__ __forceinline__ Stat join_parts(const Stat *stats, int parts, float c) {
   const int lane = threadIdx.x & 63;
-  return wave_join(lane < parts ? stats[lane] : no_logits(), c);
+  return wave_join<kEntropy>(lane < parts ? stats[lane] : no_logits(), c);
 }
 
 // One block a row.  The parts' best keys bound the k-th best from below.
@@ -381,7 +443,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(const typename 
   __shared__ TopLds l;
   const int64_t r = blockIdx.x;
   const typename D::raw *row = z + r * ld;
-  const Stat s = join_parts(po.stats + r * parts, parts, c);
+  const Stat s = join_parts<true>(po.stats + r * parts, parts, c);
   if (threadIdx.x == 0) write_row<D>(o, row, r, V, s);
   if constexpr (kTop) {
     const uint64_t *keys = po.keys + r * parts * o.k;
@@ -445,67 +507,24 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(
   });
 }
 
-// p (exp(-u) - 1 + u), from u = ln p - ln q.  Near 0 by its series, which
-// neither cancels nor depends on the rounding of q - p.
-__device__ __forceinline__ float kl_term(float p, float q, float u) {
-  if (p == 0.f) return q;
-  if (fabsf(u) < 0.5f) {
-    float h = fmaf(-u, 1.f / 40320, 1.f / 5040);
-    h = fmaf(-u, h, 1.f / 720);
-    h = fmaf(-u, h, 1.f / 120);
-    h = fmaf(-u, h, 1.f / 24);
-    h = fmaf(-u, h, 1.f / 6);
-    h = fmaf(-u, h, 0.5f);
-    return p * (u * u * h);
-  }
-  return fmaf(p, u, q - p);
-}
-
-// Both rows' statistics and what the second pass needs of them.
-struct KlRow {
-  float ms, ls, mt, lt;  // largest logit and log2 Z of the student and the teacher
-  float g;               // the gradient's factor
-  bool none, bad;        // a row that masks everything; NaN
-  float instead;         // kl where none
-};
-
-__device__ __forceinline__ KlRow kl_row(const Stat &a, const Stat &b, float g) {
-  KlRow k{a.m, log2f(a.Z), b.m, log2f(b.Z), g, empty(a) || empty(b), false, 0.f};
-  // teacher masked: nothing to match; student masked: no finite code for it
-  if (k.none)
-    k.instead = a.Z != a.Z || b.Z != b.Z ? __builtin_nanf("") : empty(b) ? 0.f : kInf;
-  return k;
-}
-
-// The chunks of both rows, two loads of each in flight.
-template <typename D, typename F>
-__device__ __forceinline__ void each_pair(const typename D::raw *s, const typename D::raw *t,
-                                          int64_t c0, int64_t c1, int64_t V, F &&f) {
-  constexpr int kAhead = 2;
-  const int64_t whole = min(c1, V / 8);
-  int64_t i = c0 + threadIdx.x;
-  for (; i + (kAhead - 1) * kThreads < whole; i += kAhead * kThreads) {
-    Eight<typename D::raw> a[kAhead], b[kAhead];
-#pragma unroll
-    for (int q = 0; q < kAhead; ++q) {
-      a[q] = load_raw<D>(s, i + q * kThreads);
-      b[q] = load_raw<D>(t, i + q * kThreads);
-    }
-#pragma unroll
-    for (int q = 0; q < kAhead; ++q) {
-      float x[8], w[8];
-      widen<D>(a[q], x);
-      widen<D>(b[q], w);
-      f(i + q * kThreads, x, w);
-    }
-  }
-  for (; i < c1; i += kThreads) {
-    float x[8], w[8];
-    load8<D>(s, i, V, -kInf, x);
-    load8<D>(t, i, V, -kInf, w);
-    f(i, x, w);
-  }
-}
+// ---------------------------------------------------------------------------
+// KL divergence.  With p and q the teacher's and the student's softmax and
+// u = log2 p - log2 q,
+//   kl = ln2 A + ln(1 + B),   A = sum p u,   B = sum (p 2^-u - p) = sum (q - p).
+// B is 0 but for rounding.  What the fp32 statistics are off by shifts all u
+// alike, by s say; A then changes by s and ln2 A + ln(1 + B) only by its square,
+// so a divergence that is small beside the logarithms keeps its digits.  u is
+// taken from the difference of the two logits, and q - p = p (2^-u - 1), the
+// gradient's factor, from u.
+//
+// A block holds its part of both rows in registers from the first pass
+// (statistics) to the second (terms and gradient), so that memory is read
+// once.  A row of several parts is several blocks' work: each publishes its
+// statistics, waits for the others' and joins them all in the parts' order.
+// Waiting is bounded: statistics that do not arrive (their block has found no
+// place on the device yet) are computed by the block that misses them, from the
+// logits, with the same operations.
+// ---------------------------------------------------------------------------
 
 struct KlArgs {
   int64_t V, ld_s, ld_t, ldd;
@@ -513,116 +532,263 @@ struct KlArgs {
   const float *weight;
   float *kl;
   Parts parts;
-  Stat *stats;      // [2, T, parts]: the student's, then the teacher's
-  float *sums;      // [T, parts]
+  // where a row has several parts:
+  uint64_t *stats;  // [2, T, parts]: m and Z of the student, then of the teacher
+  uint64_t *sums;   // [T, parts]: A and B
+  int *done;        // [T]
 };
 
-// One part of the second pass: gradient written, the terms' sum returned (in
-// every thread).
-template <typename D>
-__device__ float kl_part(const KlRow &k, const typename D::raw *s, const typename D::raw *t,
-                         typename D::raw *ds, int64_t c0, int64_t c1, const KlArgs &g, float *sh) {
-  const float c = g.scale * kLog2e;
-  const bool zero = k.none || k.g == 0.f;
-  float sum = 0.f;
-  each_pair<D>(s, t, c0, c1, g.V, [&](int64_t i, const float(&x)[8], const float(&w)[8]) {
-    float d[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float tq = fmaf(x[j] - k.ms, c, -k.ls), tp = fmaf(w[j] - k.mt, c, -k.lt);
-      const float q = exp2_hw(tq), p = exp2_hw(tp);
-      sum += kl_term(p, q, kLn2 * (tp - tq));
-      d[j] = zero ? 0.f : k.g * (q - p);
-    }
-    if (ds) store8<D>(ds, i, g.V, d);
-  });
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = sum;
-  __syncthreads();
-  sum = sh[0];
-  for (int w = 1; w < kWaves; ++w) sum += sh[w];
-  return sum;
+constexpr uint64_t kNotYet = ~0ull;  // m is never NaN, so no statistics look so
+constexpr int kPolls = 4096;
+
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  return (uint64_t)__float_as_uint(a) << 32 | __float_as_uint(b);
+}
+__device__ __forceinline__ float first_of(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
+__device__ __forceinline__ float second_of(uint64_t v) { return __uint_as_float((uint32_t)v); }
+
+__device__ __forceinline__ uint64_t peek(const uint64_t *p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// Stores v where every part of the chip sees it, and returns when it is there.
+__device__ __forceinline__ void publish(uint64_t *p, uint64_t v) {
+  const uint64_t old = __hip_atomic_exchange(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  asm volatile("" ::"v"(old) : "memory");
 }
 
+__global__ __launch_bounds__(kThreads) void kl_clear_kernel(uint64_t *words, int64_t n, int *done,
+                                                            int64_t T) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i < n) words[i] = kNotYet;
+  if (i < T) done[i] = 0;
+}
+
+struct KlLds {
+  Stat wave[2 * kWaves];
+  Stat part[2][64];
+  Stat row[2];
+  float sum[2 * kWaves];
+  uint64_t missing;
+};
+
+// Statistics of a part whose block has not delivered.
 template <typename D>
-__device__ __forceinline__ void pair_stats(const typename D::raw *s, const typename D::raw *t,
-                                           int64_t c0, int64_t c1, int64_t V, float c, Stat *sh,
+__device__ __forceinline__ void part_stats(const typename D::raw *s, const typename D::raw *t,
+                                           int64_t c0, int64_t c1, int64_t V, float c, KlLds &l,
                                            Stat &a, Stat &b) {
   a = b = no_logits();
-  each_pair<D>(s, t, c0, c1, V, [&](int64_t, const float(&x)[8], const float(&w)[8]) {
-    add(a, x, c);
-    add(b, w, c);
-  });
-  a = block_join<kThreads>(a, c, sh);
-  b = block_join<kThreads>(b, c, sh);
-}
-
-// A row a block, both passes: the second finds the row in the caches.
-template <typename D>
-__global__ __launch_bounds__(kThreads) void kl_rows_kernel(const typename D::raw *zs,
-                                                           const typename D::raw *zt,
-                                                           typename D::raw *ds, KlArgs g) {
-  __shared__ Stat sh[kWaves];
-  __shared__ float part[kWaves];
-  const int64_t r = blockIdx.x, chunks = (g.V + 7) / 8;
-  const typename D::raw *s = zs + r * g.ld_s, *t = zt + r * g.ld_t;
-  Stat a, b;
-  pair_stats<D>(s, t, 0, chunks, g.V, g.scale * kLog2e, sh, a, b);
-  const KlRow k = kl_row(a, b, (g.weight ? g.weight[r] : 1.f) * g.scale);
-  const float sum = kl_part<D>(k, s, t, ds ? ds + r * g.ldd : nullptr, 0, chunks, g, part);
-  if (threadIdx.x == 0) g.kl[r] = k.none ? k.instead : sum;
-}
-
-// The same in parts: statistics, then terms and gradient, then the terms' sum.
-template <typename D>
-__global__ __launch_bounds__(kThreads) void kl_stats_kernel(const typename D::raw *zs,
-                                                            const typename D::raw *zt, int64_t T,
-                                                            KlArgs g) {
-  __shared__ Stat sh[kWaves];
-  const int64_t r = blockIdx.x / g.parts.count;
-  const int64_t c0 = blockIdx.x % g.parts.count * g.parts.size;
-  Stat a, b;
-  pair_stats<D>(zs + r * g.ld_s, zt + r * g.ld_t, c0, min(c0 + g.parts.size, (g.V + 7) / 8), g.V,
-                g.scale * kLog2e, sh, a, b);
-  if (threadIdx.x == 0) {
-    g.stats[blockIdx.x] = a;
-    g.stats[T * g.parts.count + blockIdx.x] = b;
+  for (int64_t i = c0 + threadIdx.x; i < c1; i += kThreads) {
+    float x[8], w[8];
+    load8<D>(s, i, V, -kInf, x);
+    load8<D>(t, i, V, -kInf, w);
+    add8<false>(a, x, max8(x), c);
+    add8<false>(b, w, max8(w), c);
   }
+  __syncthreads();
+  a = block_join<false>(a, c, l.wave);
+  b = block_join<false>(b, c, l.wave + kWaves);
 }
 
-__device__ __forceinline__ KlRow kl_join(int64_t r, int64_t T, const KlArgs &g) {
-  const Stat *st = g.stats + r * g.parts.count;
-  const float c = g.scale * kLog2e;
-  const Stat a = join_parts(st, g.parts.count, c);
-  const Stat b = join_parts(st + T * g.parts.count, g.parts.count, c);
-  return kl_row(a, b, (g.weight ? g.weight[r] : 1.f) * g.scale);
-}
-
+// The rows' statistics from all parts'; every thread of the block calls it.
 template <typename D>
-__global__ __launch_bounds__(kThreads) void kl_parts_kernel(const typename D::raw *zs,
-                                                            const typename D::raw *zt,
-                                                            typename D::raw *ds, int64_t T,
-                                                            KlArgs g) {
-  __shared__ float part[kWaves];
-  const int64_t r = blockIdx.x / g.parts.count;
-  const int64_t c0 = blockIdx.x % g.parts.count * g.parts.size;
-  const float sum = kl_part<D>(kl_join(r, T, g), zs + r * g.ld_s, zt + r * g.ld_t,
-                               ds ? ds + r * g.ldd : nullptr, c0,
-                               min(c0 + g.parts.size, (g.V + 7) / 8), g, part);
-  if (threadIdx.x == 0) g.sums[blockIdx.x] = sum;
+__device__ void join_rows(const typename D::raw *s, const typename D::raw *t, int64_t r, int64_t T,
+                          const KlArgs &g, float c, KlLds &l, Stat &a, Stat &b) {
+  const int n = g.parts.count;
+  const uint64_t *sa = g.stats + r * n, *sb = g.stats + (T + r) * n;
+  for (int base = 0; base < n; base += 64) {
+    const int here = min(64, n - base);
+    if (threadIdx.x < 64) {
+      const int lane = threadIdx.x;
+      uint64_t va = 0, vb = 0;
+      bool have = lane >= here;
+      for (int poll = 0; poll < kPolls; ++poll) {
+        if (!have) {
+          va = peek(sa + base + lane);
+          vb = peek(sb + base + lane);
+          have = va != kNotYet && vb != kNotYet;
+        }
+        if (__all(have)) break;
+        __builtin_amdgcn_s_sleep(2);
+      }
+      if (have && lane < here) {
+        l.part[0][lane] = Stat{first_of(va), second_of(va), 0.f};
+        l.part[1][lane] = Stat{first_of(vb), second_of(vb), 0.f};
+      }
+      const uint64_t missing = __ballot(!have);
+      if (lane == 0) l.missing = missing;
+    }
+    __syncthreads();
+    for (uint64_t missing = l.missing; missing; missing &= missing - 1) {
+      const int p = __builtin_ctzll(missing);
+      const int64_t c0 = (base + p) * g.parts.size;
+      Stat x, y;
+      part_stats<D>(s, t, c0, min(c0 + g.parts.size, (g.V + 7) / 8), g.V, c, l, x, y);
+      if (threadIdx.x == 0) {
+        // The part's block writes its gradient, maybe over these logits, only
+        // after it has published: what it published by now goes first.
+        const uint64_t va = peek(sa + base + p), vb = peek(sb + base + p);
+        if (va != kNotYet && vb != kNotYet) {
+          x = Stat{first_of(va), second_of(va), 0.f};
+          y = Stat{first_of(vb), second_of(vb), 0.f};
+        }
+        l.part[0][p] = x;
+        l.part[1][p] = y;
+      }
+      __syncthreads();
+    }
+    if (threadIdx.x < 64) {
+      const int lane = threadIdx.x;
+      Stat x = lane < here ? l.part[0][lane] : no_logits();
+      Stat y = lane < here ? l.part[1][lane] : no_logits();
+      x = wave_join<false>(x, c);
+      y = wave_join<false>(y, c);
+      if (base > 0) {
+        x = join2(l.row[0], x, c);
+        y = join2(l.row[1], y, c);
+      }
+      if (lane == 0) l.row[0] = x, l.row[1] = y;
+    }
+    __syncthreads();
+  }
+  a = l.row[0];
+  b = l.row[1];
 }
 
-__global__ __launch_bounds__(kThreads) void kl_sum_kernel(int64_t T, KlArgs g) {
-  const int64_t r = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-  if (r >= T) return;
-  const int lane = threadIdx.x & 63;
-  float sum = lane < g.parts.count ? g.sums[r * g.parts.count + lane] : 0.f;
+template <typename D, int kChunks>
+__global__ __launch_bounds__(kThreads, 4) void kl_kernel(const typename D::raw *zs,
+                                                         const typename D::raw *zt,
+                                                         typename D::raw *ds, int64_t T, KlArgs g) {
+  using R = typename D::raw;
+  __shared__ KlLds l;
+  const int parts = g.parts.count;
+  const int64_t r = blockIdx.x / parts, V = g.V;
+  const int64_t c0 = blockIdx.x % parts * g.parts.size;
+  const int64_t c1 = min(c0 + g.parts.size, (V + 7) / 8);
+  const R *s = zs + r * g.ld_s, *t = zt + r * g.ld_t;
+  const float c = g.scale * kLog2e;
+
+  Eight<D> xs[kChunks], xt[kChunks];
+  const int whole = (int)(V / 8), first = (int)c0 + threadIdx.x, end = (int)c1;
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-  const KlRow k = kl_join(r, T, g);
-  if (lane == 0) g.kl[r] = k.none ? k.instead : sum;
+  for (int j = 0; j < kChunks; ++j) {
+    // chunks that are not there read another one and look masked
+    const int i = first + j * kThreads;
+    const uint32_t at = (uint32_t)min(i, whole - 1) * (uint32_t)sizeof(Eight<D>);
+    if (whole > 0) {
+      xs[j] = *reinterpret_cast<const Eight<D> *>(reinterpret_cast<const char *>(s) + at);
+      xt[j] = *reinterpret_cast<const Eight<D> *>(reinterpret_cast<const char *>(t) + at);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kChunks; ++j) {
+    const int i = first + j * kThreads;
+    if (i >= whole || i >= end) {
+      const int64_t some = i < end ? V : 0;
+      xs[j] = load_raw_to<D>(s, i, some, -kInf);
+      xt[j] = load_raw_to<D>(t, i, some, -kInf);
+    }
+  }
+  Stat a = no_logits(), b = no_logits();
+#pragma unroll
+  for (int j = 0; j < kChunks; ++j) {
+    if (c0 + j * kThreads >= c1) break;
+    float x[8];
+    widen<D>(xs[j], x);
+    add8<false>(a, x, max8(x), c);
+    widen<D>(xt[j], x);
+    add8<false>(b, x, max8(x), c);
+  }
+  a = block_join<false>(a, c, l.wave);
+  b = block_join<false>(b, c, l.wave + kWaves);
+  if (parts > 1) {
+    if (threadIdx.x == 0) {
+      publish(g.stats + blockIdx.x, pack2(a.m, a.Z));
+      publish(g.stats + T * parts + blockIdx.x, pack2(b.m, b.Z));
+    }
+    join_rows<D>(s, t, r, T, g, c, l, a, b);
+  }
+
+  const float gf = (g.weight ? g.weight[r] : 1.f) * g.scale;
+  const bool none = empty(a) || empty(b), zero = none || gf == 0.f;
+  const float la = log2f(a.Z), lb = log2f(b.Z);
+  const float K = fmaf(b.m - a.m, c, lb - la);
+  float A = 0.f, B = 0.f;
+#pragma unroll
+  for (int j = 0; j < kChunks; ++j) {
+    if (c0 + j * kThreads >= c1) break;
+    float x[8], w[8], d[8];
+    widen<D>(xs[j], x);
+    widen<D>(xt[j], w);
+#pragma unroll
+    for (int h = 0; h < 8; h += 4) {
+      float p[4], e[4], u[4], least = kInf, most = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        p[k] = exp2_hw(fmaf(w[h + k] - b.m, c, -lb));
+        u[k] = fmaf(w[h + k] - x[h + k], c, -K);
+        e[k] = exp2_hw(-u[k]);
+        least = fminf(least, p[k]);
+        most = fmaxf(most, e[k]);
+      }
+      if (least > 0.f && most < kInf) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          d[h + k] = fmaf(p[k], e[k], -p[k]);
+          A = fmaf(p[k], u[k], A);
+        }
+      } else {
+        // masked entries, or ones below fp32: q on its own; 0 log 0 is 0
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          d[h + k] = exp2_hw(fmaf(x[h + k] - a.m, c, -la)) - p[k];
+          A = fmaf(p[k], p[k] == 0.f ? 0.f : u[k], A);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        B += d[h + k];
+        d[h + k] = zero ? 0.f : d[h + k] * gf;
+      }
+    }
+    const int64_t i = c0 + threadIdx.x + j * kThreads;
+    if (ds && i < c1) store8<D>(ds + r * g.ldd, i, V, d);
+  }
+  A = wave_add(A);
+  B = wave_add(B);
+  if ((threadIdx.x & 63) == 0) {
+    l.sum[threadIdx.x >> 6] = A;
+    l.sum[kWaves + (threadIdx.x >> 6)] = B;
+  }
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  A = l.sum[0];
+  B = l.sum[kWaves];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) A += l.sum[w], B += l.sum[kWaves + w];
+  const int lane = threadIdx.x;
+  if (parts > 1) {
+    // the block that finishes the row adds the parts' sums
+    int last = 0;
+    if (lane == 0) {
+      publish(g.sums + blockIdx.x, pack2(A, B));
+      last = __hip_atomic_fetch_add(g.done + r, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+             parts - 1;
+    }
+    if (!__builtin_amdgcn_readfirstlane(last)) return;
+    A = B = 0.f;
+    for (int base = 0; base < parts; base += 64) {
+      const uint64_t v = base + lane < parts ? peek(g.sums + r * parts + base + lane) : 0;
+      A += wave_add(first_of(v));
+      B += wave_add(second_of(v));
+    }
+  }
+  if (lane == 0) {
+    float kl = fmaf(kLn2, A, log1pf(B));
+    kl = kl < 0.f ? 0.f : kl;  // the divergence is not: 0 is nearer to it
+    // teacher masked: nothing to match; student masked: no finite code for it
+    if (none) kl = a.Z != a.Z || b.Z != b.Z ? __builtin_nanf("") : empty(b) ? 0.f : kInf;
+    g.kl[r] = kl;
+  }
 }
 
 // Parts of a row for T rows: as many as give the device kWant blocks, of at
@@ -656,9 +822,11 @@ hipError_t launch_token_logprobs(const Rows &z, float scale, const int64_t *targ
                                  hipStream_t s) {
   const RowOut o{targets, logprob, entropy, lse, saved, k, top_logprob, top_index, scale};
   const Parts p = plan_parts(z.T, z.V, kMaxParts);
-  const PartOut po{static_cast<Stat *>(ws),
-                   reinterpret_cast<uint64_t *>(static_cast<uint8_t *>(ws) +
-                                                up16((size_t)z.T * p.count * sizeof(Stat)))};
+  PartOut po{nullptr, nullptr};
+  if (p.count > 1)
+    po = PartOut{static_cast<Stat *>(ws),
+                 reinterpret_cast<uint64_t *>(static_cast<uint8_t *>(ws) +
+                                              up16((size_t)z.T * p.count * sizeof(Stat)))};
   const float c = scale * kLog2e;
   return with_type(z.dtype, [&](auto d) {
     using D = decltype(d);
@@ -696,35 +864,69 @@ hipError_t launch_token_logprobs_backward(const Rows &z, float scale, const int6
   });
 }
 
+// Chunks of eight that a thread of the KL kernel holds of each row: 64
+// registers, or 32 bytes when there are few rows to fill the device with.
+template <typename D>
+constexpr int kl_chunks(bool few) {
+  return few ? (sizeof(typename D::raw) == 4 ? 1 : 2) : (sizeof(typename D::raw) == 4 ? 4 : 8);
+}
+
+struct KlPlan {
+  bool few;
+  Parts parts;
+};
+
+KlPlan plan_kl(int dtype, int64_t T, int64_t V) {
+  return with_type(dtype, [&](auto d) {
+    using D = decltype(d);
+    const int64_t chunks = (V + 7) / 8;
+    KlPlan p;
+    for (bool few : {false, true}) {
+      const int64_t most = (int64_t)kl_chunks<D>(few) * kThreads, n = (chunks + most - 1) / most;
+      // as even as whole turns of the block allow
+      const int64_t size = ((chunks + n - 1) / n + kThreads - 1) / kThreads * kThreads;
+      p = KlPlan{few, Parts{(int)((chunks + size - 1) / size), size}};
+      if (T * p.parts.count >= kWant / 2) break;
+    }
+    return p;
+  });
+}
+
 size_t distill_kl_workspace_bytes(int64_t T, int64_t V) {
-  const Parts p = plan_parts(T, V, kMaxParts);
-  return p.count == 1 ? 0 : up16((size_t)2 * T * p.count * sizeof(Stat)) + (size_t)T * p.count * 4;
+  // of whatever type the logits are
+  size_t most = 0;
+  for (int dtype : {AF1_SRC_F32, AF1_SRC_BF16, AF1_SRC_F16}) {
+    const size_t n = plan_kl(dtype, T, V).parts.count;
+    const size_t need = n == 1 ? 0 : (size_t)T * (n * 24 + 4);
+    most = need > most ? need : most;
+  }
+  return most;
 }
 
 hipError_t launch_distill_kl(const Rows &z, const void *teacher, int64_t ld_t, float scale,
                              const float *weight, float *kl, void *dstudent, int64_t ldd, void *ws,
                              hipStream_t s) {
-  const Parts p = plan_parts(z.T, z.V, kMaxParts);
-  const KlArgs g{z.V, z.ld, ld_t, ldd, scale, weight, kl, p, static_cast<Stat *>(ws),
-                 reinterpret_cast<float *>(static_cast<uint8_t *>(ws) +
-                                           up16((size_t)2 * z.T * p.count * sizeof(Stat)))};
+  const KlPlan plan = plan_kl(z.dtype, z.T, z.V);
+  KlArgs g{z.V, z.ld, ld_t, ldd, scale, weight, kl, plan.parts, nullptr, nullptr, nullptr};
+  const int64_t blocks = z.T * plan.parts.count;
+  if (plan.parts.count > 1) {
+    g.stats = static_cast<uint64_t *>(ws);
+    g.sums = g.stats + 2 * blocks;
+    g.done = reinterpret_cast<int *>(g.sums + blocks);
+    kl_clear_kernel<<<(unsigned)((2 * blocks + kThreads - 1) / kThreads), kThreads, 0, s>>>(
+        g.stats, 2 * blocks, g.done, z.T);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   return with_type(z.dtype, [&](auto d) {
     using D = decltype(d);
     const auto *a = static_cast<const typename D::raw *>(z.p);
     const auto *b = static_cast<const typename D::raw *>(teacher);
     auto *out = static_cast<typename D::raw *>(dstudent);
-    if (p.count == 1) {
-      kl_rows_kernel<D><<<(unsigned)z.T, kThreads, 0, s>>>(a, b, out, g);
-      return hipGetLastError();
-    }
-    const unsigned blocks = (unsigned)(z.T * p.count);
-    kl_stats_kernel<D><<<blocks, kThreads, 0, s>>>(a, b, z.T, g);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    kl_parts_kernel<D><<<blocks, kThreads, 0, s>>>(a, b, out, z.T, g);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    kl_sum_kernel<<<(unsigned)((z.T + kWaves - 1) / kWaves), kThreads, 0, s>>>(z.T, g);
+    if (plan.few)
+      kl_kernel<D, kl_chunks<D>(true)><<<(unsigned)blocks, kThreads, 0, s>>>(a, b, out, z.T, g);
+    else
+      kl_kernel<D, kl_chunks<D>(false)><<<(unsigned)blocks, kThreads, 0, s>>>(a, b, out, z.T, g);
     return hipGetLastError();
   });
 }

@@ -385,20 +385,23 @@ def test_logprobs_backward_in_place_and_strided(dtype):
 # --------------------------------------------------------------------------
 
 def kl_bound(xs, xt, scale):
-    """A term p phi(u) errs by what u = log p - log q is off, times |p - q|,
-    and by its own rounding; terms with |u| >= 1/2 are formed from p and q, so
-    they also carry the error of those."""
+    """kl = ln2 sum p u + ln(1 + sum p (2^-u - 1)).  A term p u errs by the
+    rounding of u (two roundings of |x - w| scale, one of |u|) and by p's
+    relative error; a term of the second sum by the exponential's 2u and u's
+    rounding times q, and by its sum with p; V terms of each are summed in some
+    order (V u of the absolute terms).  What the statistics are off by (eps)
+    shifts u for all, which the two sums feel in opposite ways: second order."""
     V = xs.shape[1]
     lq, lp = (np.maximum(H.log_softmax(v, scale), -200.0) for v in (xs, xt))
     p, q, u = np.exp(lp), np.exp(lq), lp - lq
-    rel = 8 * U * (4 + np.abs(lp) + np.abs(lq))
-    term = np.abs(q - p + p * u)
-    # the statistics' own error shifts every u alike, which the sum feels in
-    # second order and through the large terms
-    big = np.abs(u) >= 0.49
-    shift = softmax_eps(V)
-    err = rel * np.abs(q - p) + (rel + 2 * shift) * np.where(big, p + q + np.abs(p * u), 0)
-    return (err + (V * U + 8 * U) * term).sum(1) + 2 * shift ** 2 + 2.0 ** -126
+    gap = np.abs(np.where(np.isfinite(xs) & np.isfinite(xt), xs - xt, 0.0)) * scale
+    eps = softmax_eps(V)
+    du = 4 * U * (gap + np.abs(u) + 1)
+    rel = eps + 4 * U * np.abs(lp) + 8 * U
+    err = p * du + q * (du + 4 * U) + rel * (np.abs(p * u) + np.abs(q - p))
+    # entries that the teacher masks take q from its own exponential
+    err = err + np.where(p < 2.0 ** -100, q * (eps + 4 * U * np.abs(lq)), 0.0)
+    return (err + V * U * (np.abs(p * u) + np.abs(q - p))).sum(1) + 2 * eps ** 2 + 4 * U * U
 
 
 def check_kl(s, t, scale=1.0, w=None, **kw):
