@@ -28,31 +28,29 @@ def _need(ok, what):
 
 
 def _dense(t, name):
-    _need(isinstance(t, torch.Tensor) and t.is_cuda, f"{name} must be a GPU tensor")
-    _need(t.dtype in DENSE, f"{name} must be float32, bfloat16, float16 or int16 (bfloat16 "
-                            f"patterns), not {t.dtype}")
-    return DENSE[t.dtype]
+    """af1's type code of a dense GPU tensor."""
+    code = DENSE.get(t.dtype) if isinstance(t, torch.Tensor) and t.is_cuda else None
+    if code is None:
+        raise ValueError(f"{name} must be a GPU tensor of float32, bfloat16, float16 or int16 "
+                         "(bfloat16 patterns)")
+    return code
 
 
 def _array(t, name, device, dtype, shape):
     """Checks an optional contiguous array of a call."""
-    if t is None:
+    if t is None or (t.dtype is dtype and t.shape == shape and t.device == device
+                     and t.is_contiguous()):
         return
-    _need(isinstance(t, torch.Tensor) and t.device == device, f"{name} must be on {device}")
-    _need(t.dtype == dtype, f"{name} must be {dtype}, not {t.dtype}")
-    _need(tuple(t.shape) == tuple(shape) and t.is_contiguous(),
-          f"{name} must be contiguous of shape {tuple(shape)}, not {tuple(t.shape)}")
+    raise ValueError(f"{name} must be {dtype}, contiguous, of shape {tuple(shape)}, on {device}, not "
+                     f"{t.dtype} of shape {tuple(t.shape)} on {t.device}")
 
 
 def _workspace(ws, need, device):
+    """(workspace, its bytes)."""
     if ws is None:
-        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        return (torch.empty(need, dtype=torch.uint8, device=device), need) if need else (None, 0)
     _need(ws.device == device and ws.is_contiguous(), f"ws must be contiguous on {device}")
-    return ws
-
-
-def _bytes(ws):
-    return 0 if ws is None else ws.numel() * ws.element_size()
+    return ws, ws.numel() * ws.element_size()
 
 
 @contextlib.contextmanager
@@ -60,6 +58,18 @@ def _on(device, stream):
     """The device of the tensors and the stream that the kernels run on."""
     with torch.cuda.device(device), on_stream(stream):
         yield
+
+
+def _run(call, device, stream, *args):
+    """call(*args, stream) on the tensors' device and the given stream, or that
+    device's current one.  Entering a device and a stream costs as much as the
+    smallest kernels, so it is left out where both are current already."""
+    if stream is None:
+        index = device.index
+        if index == torch.cuda.current_device():
+            return call(*args, torch._C._cuda_getCurrentRawStream(index))
+    with _on(device, stream):
+        return call(*args, stream)
 
 
 class Fp8Matrix:
@@ -96,32 +106,41 @@ class Fp8Matrix:
         """The 8-bit form of a dense contiguous matrix."""
         dtype = _dense(src, "src")
         _need(src.dim() == 2 and src.is_contiguous(), "src must be a contiguous matrix")
+        _need(fmt in FORMATS, f"fmt must be one of {tuple(FORMATS)}, not {fmt!r}")
         rows, cols = src.shape
-        with _on(src.device, stream):
-            if out is None:
-                out = cls.empty(rows, cols, fmt, src.device)
-            _need((out.rows, out.cols, out.fmt) == (rows, cols, fmt) and out.device == src.device,
-                  f"out must be a {rows} x {cols} {fmt} matrix on {src.device}")
-            head.af1_fp8_quantize(src, dtype, rows, cols, FORMATS[fmt], out.codes, out.scales,
-                                  stream)
-        return out
+        _need(out is None or ((out.rows, out.cols, out.fmt) == (rows, cols, fmt)
+                              and out.device == src.device),
+              f"out must be a {rows} x {cols} {fmt} matrix on {src.device}")
+
+        def call(stream):
+            M = cls.empty(rows, cols, fmt, src.device) if out is None else out
+            head.af1_fp8_quantize(src, dtype, rows, cols, FORMATS[fmt], M.codes, M.scales, stream)
+            return M
+
+        return _run(call, src.device, stream)
 
     def dequantize(self, dtype=torch.bfloat16, out=None, stream=None):
         """The values that the matrix stands for."""
         _need(dtype in DENSE, f"dtype must be one of {tuple(DENSE)}, not {dtype}")
-        with _on(self.device, stream):
-            if out is None:
-                out = torch.empty((self.rows, self.cols), dtype=dtype, device=self.device)
-            _array(out, "out", self.device, dtype, (self.rows, self.cols))
-            head.af1_fp8_dequantize(self.desc, out, DENSE[dtype], stream)
-        return out
+        _array(out, "out", self.device, dtype, (self.rows, self.cols))
+
+        def call(stream):
+            dst = out
+            if dst is None:
+                dst = torch.empty((self.rows, self.cols), dtype=dtype, device=self.device)
+            head.af1_fp8_dequantize(self.desc, dst, DENSE[dtype], stream)
+            return dst
+
+        return _run(call, self.device, stream)
 
     def transpose(self, stream=None):
         """The transposed matrix; codes and scales are moved, nothing rounds."""
-        with _on(self.device, stream):
-            out = Fp8Matrix.empty(self.cols, self.rows, self.fmt, self.device)
-            head.af1_fp8_transpose(self.desc, out.codes, out.scales, stream)
-        return out
+        def call(stream):
+            T = Fp8Matrix.empty(self.cols, self.rows, self.fmt, self.device)
+            head.af1_fp8_transpose(self.desc, T.codes, T.scales, stream)
+            return T
+
+        return _run(call, self.device, stream)
 
 
 class Fp8Linear:
@@ -161,25 +180,26 @@ class Fp8Linear:
 
     def input_grad(self, dy, dx=None, ws=None, fmt="e5m2", dtype=torch.bfloat16, stream=None):
         """dx = dy W, [T, m] -> [T, n]."""
-        with _on(self.weight.device, stream):
-            WT = self.transposed(stream)
-        return _linear(WT, dy, dx, ws, fmt, dtype, stream)
+        return _linear(self.transposed(stream), dy, dx, ws, fmt, dtype, stream)
 
 
 def _linear(W, x, y, ws, fmt, dtype, stream):
-    x_dtype = _dense(x, "x")
+    x_dtype, dev = _dense(x, "x"), W.codes.device
     _need(fmt in FORMATS, f"fmt must be one of {tuple(FORMATS)}, not {fmt!r}")
-    _need(x.dim() == 2 and x.shape[1] == W.cols and x.is_contiguous() and x.device == W.device,
-          f"x must be contiguous of shape [T, {W.cols}] on {W.device}")
-    T = x.shape[0]
-    with _on(W.device, stream):
-        if y is None:
-            y = torch.empty((T, W.rows), dtype=dtype, device=x.device)
-        y_dtype = _dense(y, "y")
-        _array(y, "y", x.device, y.dtype, (T, W.rows))
-        ws = _workspace(ws, head.af1_fp8_linear_workspace_bytes(W.rows, W.cols, T), x.device)
-        head.af1_fp8_linear(W.desc, x, x_dtype, FORMATS[fmt], T, y, y_dtype, ws, _bytes(ws),
-                            stream)
+    if x.dim() != 2 or x.shape[1] != W.cols or not x.is_contiguous() or x.device != dev:
+        raise ValueError(f"x must be contiguous of shape [T, {W.cols}] on {dev}")
+    if y is not None:
+        _array(y, "y", dev, y.dtype, (x.shape[0], W.rows))
+    return _run(_linear_call, dev, stream, W, x, x_dtype, FORMATS[fmt], y, dtype, ws)
+
+
+def _linear_call(W, x, x_dtype, fmt, y, dtype, ws, stream):
+    T, dev = x.shape[0], x.device
+    if y is None:
+        y = torch.empty((T, W.rows), dtype=dtype, device=dev)
+    ws, size = _workspace(ws, head.af1_fp8_linear_workspace_bytes(W.rows, W.cols, T)
+                          if ws is None else 0, dev)
+    head.af1_fp8_linear(W.desc, x, x_dtype, fmt, T, y, _dense(y, "y"), ws, size, stream)
     return y
 
 
@@ -208,20 +228,30 @@ class TokenLogprobs(NamedTuple):
 def token_logprobs(logits, targets=None, k=0, scale=1.0, ws=None, stream=None):
     """Log probabilities of the given tokens under softmax(scale * logits), the
     entropy, and the k most likely tokens (af1_token_logprobs)."""
-    dtype, T, V, ld = _logits(logits, "logits")
-    dev = logits.device
+    rows, dev = _logits(logits, "logits"), logits.device
+    T = rows[1]
     _array(targets, "targets", dev, torch.int64, (T,))
     _need(0 <= k <= head.AF1_HEAD_MAX_TOP, f"k must be in 0..{head.AF1_HEAD_MAX_TOP}, not {k}")
-    with _on(dev, stream):
-        # one block: entropy, lse, logprob and alternatives behind the saved rows
-        buf = torch.empty((7 + k) * T, dtype=torch.float32, device=dev)
-        saved, entropy, lse = buf[:4 * T].view(T, 4), buf[4 * T:5 * T], buf[5 * T:6 * T]
-        logprob = buf[6 * T:7 * T] if targets is not None else None
-        top = buf[7 * T:].view(T, k) if k else None
-        index = torch.empty((T, k), dtype=torch.int64, device=dev) if k else None
-        ws = _workspace(ws, head.af1_token_logprobs_workspace_bytes(T, V, k), dev)
-        head.af1_token_logprobs(logits, dtype, T, V, ld, scale, targets, logprob, entropy, lse, k,
-                                top, index, saved, ws, _bytes(ws), stream)
+    return _run(_logprobs_call, dev, stream, logits, rows, targets, k, scale, ws)
+
+
+def _logprobs_call(logits, rows, targets, k, scale, ws, stream):
+    dtype, T, V, ld = rows
+    dev = logits.device
+    # the saved rows first: they are 16 bytes each and aligned so
+    saved, entropy, lse, logprob, top = torch.empty(
+        (7 + k) * T, dtype=torch.float32, device=dev).split((4 * T, T, T, T, k * T))
+    saved, index = saved.view(T, 4), None
+    if targets is None:
+        logprob = None
+    if k:
+        top, index = top.view(T, k), torch.empty((T, k), dtype=torch.int64, device=dev)
+    else:
+        top = None
+    ws, size = _workspace(ws, head.af1_token_logprobs_workspace_bytes(T, V, k)
+                          if ws is None else 0, dev)
+    head.af1_token_logprobs(logits, dtype, T, V, ld, scale, targets, logprob, entropy, lse, k, top,
+                            index, saved, ws, size, stream)
     return TokenLogprobs(logprob, entropy, lse, top, index, saved)
 
 
@@ -237,11 +267,14 @@ def token_logprobs_backward(logits, targets, result, g_logprob=None, g_entropy=N
     _array(g_entropy, "g_entropy", dev, torch.float32, (T,))
     _array(result.saved, "result.saved", dev, torch.float32, (T, 4))
     _need(g_logprob is None or targets is not None, "g_logprob needs targets")
-    with _on(dev, stream):
-        dlogits, ldd = _gradient(dlogits, logits)
+
+    def call(stream):
+        out, ldd = _gradient(dlogits, logits)
         head.af1_token_logprobs_backward(logits, dtype, T, V, ld, scale, targets, result.saved,
-                                         g_logprob, g_entropy, dlogits, ldd, stream)
-    return dlogits
+                                         g_logprob, g_entropy, out, ldd, stream)
+        return out
+
+    return _run(call, dev, stream)
 
 
 def _gradient(out, logits):
@@ -264,15 +297,18 @@ def distill_kl(student, teacher, scale=1.0, weight=None, grad=True, dstudent=Non
     _need(teacher.shape == student.shape and t_dtype == dtype and teacher.device == dev,
           "student and teacher must have one shape, type and device")
     _array(weight, "weight", dev, torch.float32, (T,))
-    with _on(dev, stream):
-        kl = torch.empty(T, dtype=torch.float32, device=dev)
-        ldd = 0
+
+    def call(stream):
+        kl, out, ldd = torch.empty(T, dtype=torch.float32, device=dev), None, 0
         if grad or dstudent is not None:
-            dstudent, ldd = _gradient(dstudent, student)
-        ws = _workspace(ws, head.af1_distill_kl_workspace_bytes(T, V), dev)
-        head.af1_distill_kl(student, teacher, dtype, T, V, ld_s, ld_t, scale, weight, kl, dstudent,
-                            ldd, ws, _bytes(ws), stream)
-    return kl, dstudent
+            out, ldd = _gradient(dstudent, student)
+        wk, size = _workspace(ws, head.af1_distill_kl_workspace_bytes(T, V) if ws is None else 0,
+                              dev)
+        head.af1_distill_kl(student, teacher, dtype, T, V, ld_s, ld_t, scale, weight, kl, out, ldd,
+                            wk, size, stream)
+        return kl, out
+
+    return _run(call, dev, stream)
 
 
 def reconstruction_step(layer, output, x, teacher, weight=None, scale=1.0, grads=None,
