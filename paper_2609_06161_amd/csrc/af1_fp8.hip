@@ -9,6 +9,8 @@
 // outputs over 64 (128) columns; a lane's operand is 32 bytes of one row.
 // Which columns those are is free as long as both operands agree, since all of
 // a block's columns share one scale.
+#include <type_traits>
+
 #include "af1_head_device.h"
 #include "af1_head_internal.h"
 
@@ -194,8 +196,20 @@ __host__ __device__ inline XTiles x_tiles(void *ws, int64_t n, int64_t T) {
   return XTiles{static_cast<uint8_t *>(ws), static_cast<uint8_t *>(ws) + tiles * kTileBytes};
 }
 
+// Up to 16 tokens instead as operands of 16 x 16 pieces: two KiB a column block,
+// [2][64 lanes][16 bytes] (the two halves of a lane's 32 columns), and behind
+// all blocks 16 scales a block.
+__device__ __forceinline__ int operand_at(int J, int t, int k) {
+  // columns 8 k .. of a block belong to half k / 8, lane group (k / 2) mod 4
+  return J * 2048 + (k >> 3) * 1024 + ((k >> 1 & 3) * 16 + t) * 16 + (k & 1) * 8;
+}
+
+inline size_t x_tile_bytes(int64_t n, int64_t T) {
+  return (size_t)blocks_up(T) * blocks_up(n) * (kTileBytes + kBlk);
+}
+
 // Sixteen lanes a token and column block, eight columns a lane.
-template <typename D, int kFormat>
+template <typename D, int kFormat, bool kOperands>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const typename D::raw *x, int64_t T,
                                                             int64_t n, XTiles out) {
   const int64_t C = (n + kBlk - 1) / kBlk;
@@ -210,26 +224,32 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const typename D::ra
 #pragma unroll
     for (int off = 8; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 16));
     const int e = block_exponent<kFormat>(amax);
+    const uint2 codes = encode8<kFormat>(v, pow2(-e));
+    if constexpr (kOperands) {
+      *reinterpret_cast<uint2 *>(out.codes + operand_at((int)J, (int)t, k)) = codes;
+      if (k == 0) out.codes[C * 2048 + J * 16 + t] = (uint8_t)(e + 127);
+      continue;
+    }
     const int64_t tile = t / kBlk * C + J;
     const int row = (int)(t % kBlk);
-    *reinterpret_cast<uint2 *>(out.codes + tile * kTileBytes + row * kBlk + k * 8) =
-        encode8<kFormat>(v, pow2(-e));
+    *reinterpret_cast<uint2 *>(out.codes + tile * kTileBytes + row * kBlk + k * 8) = codes;
     if (k == 0) out.scales[tile * kBlk + (row & 31) * 4 + (row >> 5)] = (uint8_t)(e + 127);
   }
 }
 
-// The values of a lane's 32 codes, for four matrix instructions.
+// The values of a lane's 32 codes at a power-of-two scale, for four matrix
+// instructions.
 template <int kFormat>
-__device__ __forceinline__ void to_bf16(v8i w, bf8v (&out)[4]) {
+__device__ __forceinline__ void to_bf16(v8i w, float scale, bf8v (&out)[4]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     bf2v lo, hi;
     if constexpr (kFormat == AF1_FP8_E4M3) {
-      lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.f, false);
-      hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.f, true);
+      lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, false);
+      hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, true);
     } else {
-      lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w[i], 1.f, false);
-      hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w[i], 1.f, true);
+      lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w[i], scale, false);
+      hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w[i], scale, true);
     }
     const int j = (i & 1) * 4;
     out[i >> 1][j] = lo[0];
@@ -238,6 +258,17 @@ __device__ __forceinline__ void to_bf16(v8i w, bf8v (&out)[4]) {
     out[i >> 1][j + 3] = hi[1];
   }
 }
+
+// Whether a scale byte's power of two may go into the bfloat16 values.  With
+// both scales within 2^-50 .. 2^50 those are normal (a code is at least 2^-16)
+// and so are their products beside a block's largest, which is at least
+// 2^(16 - 100) in e4m3 and 2^(30 - 100) in e5m2: nothing is flushed that fp32
+// sums would keep.  Outside, a block is summed without scales and added at
+// its own.
+__device__ __forceinline__ bool plain_scale(int byte) { return (unsigned)(byte - 77) <= 100u; }
+
+// 2^(byte - 127) of a plain scale byte.
+__device__ __forceinline__ float scale_of(int byte) { return __uint_as_float((uint32_t)byte << 23); }
 
 // acc += products of 64 columns at the scales (E8M0): W's is byte 0 of sw, the
 // tokens' byte kByte of sx.
@@ -307,6 +338,12 @@ __device__ __forceinline__ void copy16(i32x4 r, uint8_t *dst, int voff, int soff
                : "memory");
 }
 
+// 16 bytes a lane from the lane's own address into 64 chunks at dst.
+__device__ __forceinline__ void copy16_from(const void *src, uint8_t *dst) {
+  const uint32_t m = (uint32_t)(size_t)(lds_void *)dst;
+  asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(m) : "memory");
+}
+
 // One dword, or one byte, a lane from the lane's own address into 64 dwords at
 // dst.
 __device__ __forceinline__ void copy4(const void *src, uint8_t *dst) {
@@ -336,6 +373,8 @@ struct Tile {
   static constexpr int kCopies = kCodes / 1024 / kWaves;  // a wave and step, and two of scales
   static constexpr int kOutRow = kFR * 64 + 16;  // LDS bytes of a token's bf16 outputs
   static constexpr int kOutLds = kWaves * 32 * kOutRow;
+  // waves a SIMD that the registers have to leave room for
+  static constexpr int kResident = kTW * kTX > 128 * 128 ? 1 : 2;
   static constexpr int kLds = kStages * kStage > kOutLds ? kStages * kStage : kOutLds;
   static_assert(kCodes % (1024 * kWaves) == 0 && kTW % 16 == 0 && kTX % 16 == 0);
   static_assert((kStages & (kStages - 1)) == 0 && kLds <= 160 * 1024);
@@ -348,11 +387,12 @@ struct LinearArgs {
   int C;             // column blocks
   int R, X;          // 128-row blocks of W and of the tokens
   int nW, nX;        // tiles
-  void *y;
+  int splits;        // ranges of column blocks
+  void *y;           // or [splits][T][m] fp32 partial sums, where there are several
 };
 
 template <typename TT, int kWFormat, int kXFormat, int kOut>
-__global__ __launch_bounds__(TT::kThreads) void tile_kernel(LinearArgs g) {
+__global__ __launch_bounds__(TT::kThreads, TT::kResident) void tile_kernel(LinearArgs g) {
   constexpr int kFR = TT::kFR, kFC = TT::kFC, kS = TT::kStages;
   extern __shared__ uint8_t lds[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -360,10 +400,13 @@ __global__ __launch_bounds__(TT::kThreads) void tile_kernel(LinearArgs g) {
   // workgroups of one XCD (blockIdx mod 8) take a contiguous range of tiles,
   // token tiles fastest, so that they share rows of W in their L2
   const int total = g.nW * g.nX;
-  int L = blockIdx.x;
+  const int part = blockIdx.x / total;
+  int L = blockIdx.x % total;
   if ((total & 7) == 0) L = (L & 7) * (total >> 3) + (L >> 3);
   const int w0 = L / g.nX * TT::kTW, x0 = L % g.nX * TT::kTX;  // first row and token
   const int C = g.C;
+  // this range's blocks
+  const int J0 = (int)((int64_t)C * part / g.splits), J1 = (int)((int64_t)C * (part + 1) / g.splits);
 
   // copy roles: piece p = wave kCopies + q is sixteen tile rows, W's first
   const int64_t band = (int64_t)C * kTileBytes;  // bytes of 128 rows
@@ -392,7 +435,7 @@ __global__ __launch_bounds__(TT::kThreads) void tile_kernel(LinearArgs g) {
   constexpr int kCopies = TT::kCopies + 2;
   auto copy = [&](int s, int k) {
     uint8_t *st = lds + (s & (kS - 1)) * TT::kStage;
-    const int J = s >> 1, p = wave * TT::kCopies + k;
+    const int J = J0 + (s >> 1), p = wave * TT::kCopies + k;
     if (k < TT::kCopies)
       copy16(16 * p < TT::kTW ? wr : xr, st + p * 1024, voff,
              soff[k < TT::kCopies ? k : 0] + J * (int)kTileBytes + (s & 1) * 64);
@@ -428,61 +471,72 @@ __global__ __launch_bounds__(TT::kThreads) void tile_kernel(LinearArgs g) {
   };
 
   v16f acc[kFR][kFC] = {};
-  v16f tmp[kFR][kFC];  // a block's sums, for outputs in fp32
-  auto product = [&](const Operands &o, bool second, int i, int j) {
-    if constexpr (kOut == AF1_SRC_BF16) {
-      // which byte holds a piece's scale is part of the instruction
-      if (j == 0) acc[i][0] = mfma_scaled<kWFormat, kXFormat, 0>(o.a[i], o.b[0], acc[i][0], o.sw, o.sx);
-      if constexpr (kFC > 1)
-        if (j == 1)
-          acc[i][1] = mfma_scaled<kWFormat, kXFormat, 1>(o.a[i], o.b[1], acc[i][1], o.sw, o.sx);
-      if constexpr (kFC > 2) {
-        if (j == 2)
-          acc[i][2] = mfma_scaled<kWFormat, kXFormat, 2>(o.a[i], o.b[2], acc[i][2], o.sw, o.sx);
-        if (j == 3)
-          acc[i][3] = mfma_scaled<kWFormat, kXFormat, 3>(o.a[i], o.b[3], acc[i][3], o.sw, o.sx);
-      }
-    } else {
-      bf8v a[4], b[4];
-      to_bf16<kWFormat>(o.a[i], a);
-      to_bf16<kXFormat>(o.b[j], b);
-      v16f t = second ? tmp[i][j] : v16f{};
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[q], b[q], t, 0, 0, 0);
-      tmp[i][j] = t;
-      if (second) {
-        const int e = o.sw + (o.sx >> (8 * j) & 255) - 254;
-#pragma unroll
-        for (int q = 0; q < 16; ++q) acc[i][j][q] += ldexpf(t[q], e);
-      }
+  auto product8 = [&](const Operands &o, int i, int j) {
+    // which byte holds a piece's scale is part of the instruction
+    if (j == 0) acc[i][0] = mfma_scaled<kWFormat, kXFormat, 0>(o.a[i], o.b[0], acc[i][0], o.sw, o.sx);
+    if constexpr (kFC > 1)
+      if (j == 1)
+        acc[i][1] = mfma_scaled<kWFormat, kXFormat, 1>(o.a[i], o.b[1], acc[i][1], o.sw, o.sx);
+    if constexpr (kFC > 2) {
+      if (j == 2)
+        acc[i][2] = mfma_scaled<kWFormat, kXFormat, 2>(o.a[i], o.b[2], acc[i][2], o.sw, o.sx);
+      if (j == 3)
+        acc[i][3] = mfma_scaled<kWFormat, kXFormat, 3>(o.a[i], o.b[3], acc[i][3], o.sw, o.sx);
     }
   };
+  auto x_scale = [&](const Operands &o, int j) { return o.sx >> (8 * j) & 255; };
 
   // Step s: its products, and between them the copies of step s + kStages and
   // the reads of step s + 1, the reads in the first half so that the barrier
   // does not wait for them.  A burst of copies in front of the products keeps
   // the wave's issue waiting behind the other waves' bursts.
   constexpr int kProducts = kFR * kFC;
-  auto step = [&](int s, const Operands &o, Operands &next, bool second, bool more, bool last) {
+  auto between = [&](int p, int s, Operands &next, bool more, bool last) {
+    constexpr int kHalf = kProducts > 1 ? kProducts / 2 : 1;
+    if (!last && p < kHalf)
 #pragma unroll
-    for (int p = 0; p < kProducts; ++p) {
-      constexpr int kHalf = kProducts > 1 ? kProducts / 2 : 1;
-      if (!last && p < kHalf)
+      for (int k = p * kReads / kHalf; k < (p + 1) * kReads / kHalf; ++k) read(s + 1, k, next);
+    if (more)
 #pragma unroll
-        for (int k = p * kReads / kHalf; k < (p + 1) * kReads / kHalf; ++k) read(s + 1, k, next);
-      if (more)
+      for (int k = p * kCopies / kProducts; k < (p + 1) * kCopies / kProducts; ++k)
+        copy(s + kS, k);
+  };
+  auto step = [&](auto plain, int s, const Operands &o, Operands &next, bool more, bool last) {
+    if constexpr (kOut == AF1_SRC_BF16) {
 #pragma unroll
-        for (int k = p * kCopies / kProducts; k < (p + 1) * kCopies / kProducts; ++k)
-          copy(s + kS, k);
-      product(o, second, p / kFC, p % kFC);
-      if constexpr (kOut == AF1_SRC_BF16) __builtin_amdgcn_sched_barrier(0);
+      for (int p = 0; p < kProducts; ++p) {
+        between(p, s, next, more, last);
+        product8(o, p / kFC, p % kFC);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+      constexpr bool kPlain = decltype(plain)::value;
+      bf8v b[kFC][4], a[4];
+#pragma unroll
+      for (int j = 0; j < kFC; ++j)
+        to_bf16<kXFormat>(o.b[j], kPlain ? scale_of(x_scale(o, j)) : 1.f, b[j]);
+#pragma unroll
+      for (int p = 0; p < kProducts; ++p) {
+        const int i = p / kFC, j = p % kFC;
+        if (j == 0) to_bf16<kWFormat>(o.a[i], kPlain ? scale_of(o.sw) : 1.f, a);
+        between(p, s, next, more, last);
+        v16f t = kPlain ? acc[i][j] : v16f{};
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[q], b[j][q], t, 0, 0, 0);
+        if constexpr (kPlain) {
+          acc[i][j] = t;
+        } else {
+#pragma unroll
+          for (int q = 0; q < 16; ++q) acc[i][j][q] += ldexpf(t[q], o.sw + x_scale(o, j) - 254);
+        }
+      }
     }
   };
 
   // copies of the steps behind the next one
   constexpr int kAhead = (kS - 2) * kCopies;
-  const int steps = 2 * C;
+  const int blocks = J1 - J0, steps = 2 * blocks;
   for (int s = 0; s < min(kS, steps); ++s)
 #pragma unroll
     for (int k = 0; k < kCopies; ++k) copy(s, k);
@@ -490,29 +544,53 @@ __global__ __launch_bounds__(TT::kThreads) void tile_kernel(LinearArgs g) {
   Operands o0, o1;
 #pragma unroll
   for (int k = 0; k < kReads; ++k) read(0, k, o0);
-  int J = 0;
-  for (; 2 * J + 1 + kS < steps; ++J) {
-    step_barrier<kAhead>();
-    step(2 * J, o0, o1, false, true, false);
-    step_barrier<kAhead>();
-    step(2 * J + 1, o1, o0, true, true, false);
-  }
-  // nothing more to copy: what is left has been on its way for long
-  for (; J < C - 1; ++J) {
+  auto run = [&](auto plain) {
+    int J = 0;
+    for (; 2 * J + 1 + kS < steps; ++J) {
+      step_barrier<kAhead>();
+      step(plain, 2 * J, o0, o1, true, false);
+      step_barrier<kAhead>();
+      step(plain, 2 * J + 1, o1, o0, true, false);
+    }
+    // nothing more to copy: what is left has been on its way for long
+    for (; J < blocks - 1; ++J) {
+      step_barrier<0>();
+      step(plain, 2 * J, o0, o1, false, false);
+      step_barrier<0>();
+      step(plain, 2 * J + 1, o1, o0, false, false);
+    }
     step_barrier<0>();
-    step(2 * J, o0, o1, false, false, false);
+    step(plain, 2 * J, o0, o1, false, false);
     step_barrier<0>();
-    step(2 * J + 1, o1, o0, true, false, false);
+    step(plain, 2 * J + 1, o1, o0, false, true);
+  };
+  if constexpr (kOut == AF1_SRC_BF16) {
+    run(std::true_type{});
+  } else {
+    // every scale that this tile meets
+    static_assert(kOut == AF1_SRC_BF16 || TT::kTX <= kBlk);
+    bool odd = false;
+    for (int k = 0; k < (TT::kTW + 127) / 128; ++k)
+      for (int J = J0 + threadIdx.x; J < J1; J += TT::kThreads)
+        odd |= !plain_scale(g.wscales[(int64_t)min(wb0 + k, g.R - 1) * C + J]);
+    const uint8_t *xt = g.x.scales + (int64_t)xb0 * C * kBlk;
+    for (int at = J0 * 32 + threadIdx.x; at < J1 * 32; at += TT::kThreads) {
+      // four tokens' bytes; those behind T are not set
+      const uint32_t v = reinterpret_cast<const uint32_t *>(xt)[at];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        odd |= (int64_t)xb0 * kBlk + 32 * k + (at & 31) < g.T && !plain_scale(v >> (8 * k) & 255);
+    }
+    if (__syncthreads_or(odd))
+      run(std::false_type{});
+    else
+      run(std::true_type{});
   }
-  step_barrier<0>();
-  step(2 * J, o0, o1, false, false, false);
-  step_barrier<0>();
-  step(2 * J + 1, o1, o0, true, false, true);
 
   // Outputs.  A lane holds, for its token, four consecutive rows of W in each
   // four accumulators.
-  if constexpr (kOut == AF1_SRC_F32) {
-    float *y = static_cast<float *>(g.y);
+  if (kOut == AF1_SRC_F32 || g.splits > 1) {
+    float *y = static_cast<float *>(g.y) + part * g.T * g.m;
 #pragma unroll
     for (int j = 0; j < kFC; ++j) {
       const int64_t t = x0 + tok0 + 32 * j + r;
@@ -566,21 +644,37 @@ __global__ __launch_bounds__(TT::kThreads) void tile_kernel(LinearArgs g) {
   }
 }
 
+// acc += the products of 128 columns of 16 rows of W and 16 tokens.
+template <int kWFormat, int kXFormat, int kOut>
+__device__ __forceinline__ v4f mul_block(v8i w, v8i x, v4f acc, int sw, int sx) {
+  if constexpr (kOut == AF1_SRC_BF16)
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc, kWFormat, kXFormat, 0, sw, 0,
+                                                            sx);
+  // summed from zero and added at the block's scale: these forms wait for memory
+  bf8v a[4], b[4];
+  to_bf16<kWFormat>(w, 1.f, a);
+  to_bf16<kXFormat>(x, 1.f, b);
+  v4f s = {};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[k], b[k], s, 0, 0, 0);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) acc[k] += ldexpf(s[k], sw + sx - 254);
+  return acc;
+}
+
 // ---------------------------------------------------------------------------
-// Few tokens.  The weight is read once whatever the tokens, so this form is
-// about reading it: a workgroup computes 16 kFR rows of W for up to 16 kNT
-// tokens, its waves take every kWaves-th column block, each streams its rows'
-// codes from memory straight into operands (lane q of a row's four: 16 columns
-// at 16 q and 16 at 64 + q 16, so that one load covers 64 bytes of a row), and
-// the waves' sums are added in LDS in the waves' order.  Up to 16 tokens a
-// wave rounds its own blocks of x to 8 bits in registers, which is one launch
-// and no workspace.  More tokens are rounded by a launch of their own.
+// 17 to 32 tokens of weights with too few rows to fill the device with tiles.
+// A workgroup computes 16 rows of W; its waves take every kFewWaves-th column
+// block, stream its codes from memory straight into operands (lane q of a
+// row's four: 16 columns at 16 q and 16 at 64 + 16 q, so that one load covers
+// 64 bytes of a row), and their sums are added in LDS in the waves' order: all
+// of a row's columns at once without a second launch.
 // ---------------------------------------------------------------------------
 
 struct FewArgs {
   const uint8_t *wcodes, *wscales;
-  const void *x;   // dense, or
-  XTiles xt;       // rounded
+  const void *x;  // dense
+  XTiles xt;      // rounded
   int T;
   int64_t m, n;
   void *y;
@@ -594,104 +688,40 @@ __device__ __forceinline__ v8i operand(const RowCodes &c) {
   return v8i{c.lo[0], c.lo[1], c.lo[2], c.lo[3], c.hi[0], c.hi[1], c.hi[2], c.hi[3]};
 }
 
-template <typename D>
-struct DenseRow {
-  Eight<D> v[4];
-};
+constexpr int kFewWaves = 8;
 
-template <typename D, int kXFormat, int kWFormat, int kOut, int kFR, int kNT, int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs g) {
-  constexpr bool kDense = kNT == 1;
-  extern __shared__ float sums[];  // [kWaves][kFR][kNT][64][4]
+template <int kXFormat, int kWFormat, int kOut>
+__global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewArgs g) {
+  __shared__ v4f sums[kFewWaves][2][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
-  const int64_t n = g.n;
-  const int C = (int)((n + kBlk - 1) / kBlk);
-  const int64_t row0 = (int64_t)blockIdx.x * 16 * kFR;
+  const int C = (int)((g.n + kBlk - 1) / kBlk);
+  const int64_t row0 = (int64_t)blockIdx.x * 16;
   const uint8_t *w = g.wcodes + row0 / kBlk * C * kTileBytes + (row0 % kBlk + r) * kBlk + q * 16;
   const uint8_t *wsc = g.wscales + row0 / kBlk * C;
-  const typename D::raw *xr = static_cast<const typename D::raw *>(g.x) + (int64_t)r * n + q * 16;
+  const uint8_t *x = g.xt.codes + r * kBlk + q * 16, *xsc = g.xt.scales + r * 4;
 
   struct Block {
-    RowCodes w[kFR];
-    int sw;
-    DenseRow<D> d;         // kDense
-    RowCodes x[kNT];       // otherwise
-    int sx[kNT];
+    RowCodes w, x[2];
+    int sw, sx[2];
   };
   auto load = [&](int J, Block &b) {
-#pragma unroll
-    for (int i = 0; i < kFR; ++i) {
-      const i32x4 *p = reinterpret_cast<const i32x4 *>(w + J * kTileBytes + i * 16 * kBlk);
-      b.w[i] = RowCodes{p[0], p[4]};
-    }
+    const i32x4 *p = reinterpret_cast<const i32x4 *>(w + J * kTileBytes);
+    b.w = RowCodes{p[0], p[4]};
     b.sw = wsc[J];
-    if constexpr (kDense) {
-      const typename D::raw *p = xr + (int64_t)J * kBlk;
-      const int64_t left = n - (int64_t)J * kBlk - q * 16;  // columns from here to the end
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int at = (c & 1) * 8 + (c >> 1) * 64;
-        b.d.v[c] = load_raw_to<D>(p + at, 0, r < g.T ? left - at : 0, 0.f);
-      }
-    } else {
-#pragma unroll
-      for (int t = 0; t < kNT; ++t) {
-        const int row = 16 * t + r;
-        const i32x4 *p = reinterpret_cast<const i32x4 *>(g.xt.codes + J * kTileBytes + row * kBlk + q * 16);
-        b.x[t] = RowCodes{p[0], p[4]};
-        b.sx[t] = g.xt.scales[J * kBlk + (row & 31) * 4 + (row >> 5)];
-      }
+    for (int t = 0; t < 2; ++t) {
+      p = reinterpret_cast<const i32x4 *>(x + J * kTileBytes + t * 16 * kBlk);
+      b.x[t] = RowCodes{p[0], p[4]};
+      b.sx[t] = xsc[J * kBlk + t * 64];
     }
   };
-
-  v4f acc[kFR][kNT] = {};
-  auto multiply = [&](Block &b) {
-    if constexpr (kDense) {
-      float v[4][8], amax = 0.f;
+  v4f acc[2] = {};
+  auto multiply = [&](const Block &b) {
+    const v8i a = operand(b.w);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        widen<D>(b.d.v[c], v[c]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_abs(v[c][i]));
-      }
-      // the token's four lanes
-      amax = fmaxf(amax, __shfl_xor(amax, 16, 64));
-      amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
-      const int e = block_exponent<kXFormat>(amax);
-      const float inv = pow2(-e);
-      const uint2 c0 = encode8<kXFormat>(v[0], inv), c1 = encode8<kXFormat>(v[1], inv);
-      const uint2 c2 = encode8<kXFormat>(v[2], inv), c3 = encode8<kXFormat>(v[3], inv);
-      b.x[0] = RowCodes{i32x4{(int)c0.x, (int)c0.y, (int)c1.x, (int)c1.y},
-                        i32x4{(int)c2.x, (int)c2.y, (int)c3.x, (int)c3.y}};
-      b.sx[0] = e + 127;
-    }
-    if constexpr (kOut == AF1_SRC_BF16) {
-#pragma unroll
-      for (int i = 0; i < kFR; ++i)
-#pragma unroll
-        for (int t = 0; t < kNT; ++t)
-          acc[i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-              operand(b.w[i]), operand(b.x[t]), acc[i][t], kWFormat, kXFormat, 0, b.sw, 0, b.sx[t]);
-    } else {
-      bf8v xb[kNT][4];
-#pragma unroll
-      for (int t = 0; t < kNT; ++t) to_bf16<kXFormat>(operand(b.x[t]), xb[t]);
-#pragma unroll
-      for (int i = 0; i < kFR; ++i) {
-        bf8v a[4];
-        to_bf16<kWFormat>(operand(b.w[i]), a);
-#pragma unroll
-        for (int t = 0; t < kNT; ++t) {
-          v4f s = {};
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[k], xb[t][k], s, 0, 0, 0);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) acc[i][t][k] += ldexpf(s[k], b.sw + b.sx[t] - 254);
-        }
-      }
-    }
+    for (int t = 0; t < 2; ++t)
+      acc[t] = mul_block<kWFormat, kXFormat, kOut>(a, operand(b.x[t]), acc[t], b.sw, b.sx[t]);
   };
 
   // the next block is on its way while this one is multiplied
@@ -699,56 +729,54 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(FewArgs g) {
   int J = wave;
   if (J < C) load(J, b0);
   while (J < C) {
-    if (J + kWaves < C) load(J + kWaves, b1);
+    if (J + kFewWaves < C) load(J + kFewWaves, b1);
     multiply(b0);
-    J += kWaves;
+    J += kFewWaves;
     if (J >= C) break;
-    if (J + kWaves < C) load(J + kWaves, b0);
+    if (J + kFewWaves < C) load(J + kFewWaves, b0);
     multiply(b1);
-    J += kWaves;
+    J += kFewWaves;
   }
-
-  constexpr int kPiece = 256;  // sums of a 16 x 16 piece
-#pragma unroll
-  for (int i = 0; i < kFR; ++i)
-#pragma unroll
-    for (int t = 0; t < kNT; ++t)
-      *reinterpret_cast<v4f *>(sums + ((wave * kFR + i) * kNT + t) * kPiece + lane * 4) = acc[i][t];
+  sums[wave][0][lane] = acc[0];
+  sums[wave][1][lane] = acc[1];
   __syncthreads();
-  // entry o: row o mod 16 kFR of the token o / 16 kFR
-  for (int o = threadIdx.x; o < 16 * kFR * g.T; o += 64 * kWaves) {
-    const int row = o % (16 * kFR), t = o / (16 * kFR);
-    if (row0 + row >= g.m) continue;
-    const int at = ((row >> 4) * kNT + (t >> 4)) * kPiece + ((row & 15) >> 2) * 64 + (t & 15) * 4 + (row & 3);
-    float s = sums[at];
+  // thread o: row o mod 16 of the token o / 16
+  const int row = threadIdx.x & 15, t = threadIdx.x >> 4;
+  if (t >= g.T || row0 + row >= g.m) return;
+  float s = 0.f;
 #pragma unroll
-    for (int k = 1; k < kWaves; ++k) s += sums[at + k * kFR * kNT * kPiece];
-    const int64_t out = (int64_t)t * g.m + row0 + row;
-    if constexpr (kOut == AF1_SRC_F32)
-      static_cast<float *>(g.y)[out] = s;
-    else
-      static_cast<uint16_t *>(g.y)[out] = f32_to_bf16(s);
-  }
+  for (int k = 0; k < kFewWaves; ++k) s += sums[k][t >> 4][(row >> 2) * 16 + (t & 15)][row & 3];
+  const int64_t out = (int64_t)t * g.m + row0 + row;
+  if constexpr (kOut == AF1_SRC_F32)
+    static_cast<float *>(g.y)[out] = s;
+  else
+    static_cast<uint16_t *>(g.y)[out] = f32_to_bf16(s);
 }
 
 // ---------------------------------------------------------------------------
 // Up to 16 tokens.  x rounded to 8 bits stays in LDS as operands, two KiB a
-// column block, and each wave streams strips of 16 rows of W past it.  A ring
+// column block, and each wave streams strips of 16 rows of W past it.  Every
+// workgroup needs all of x: few pieces it rounds itself (one launch, no
+// workspace), more are rounded by a launch in front (kOwnPieces).  A ring
 // of kRing blocks is in flight a wave, across the ends of strips: memory sees
 // one unbroken stream.  When there are fewer strips than waves, kSplit waves
 // share a strip, every kSplit-th block each, and add their sums in LDS in
-// order.
+// order; rows too long for LDS are taken that way too, a chunk of columns at a
+// time.
 // ---------------------------------------------------------------------------
 
 constexpr int kStripWaves = 8;
+constexpr int kStripBlocks = 72;  // column blocks that LDS holds whole
+constexpr int kStripChunk = 64;   // and as many at a time of longer rows
 
 template <typename D, int kXFormat, int kWFormat, int kOut, int kSplit>
 __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(FewArgs g) {
   constexpr int kRing = 8, kStrips = kStripWaves / kSplit;  // strips at a time
-  extern __shared__ uint8_t lds[];  // operands [C][2][64][16], scales [C][16], sums
+  extern __shared__ uint8_t lds[];  // operands [held][2][64][16], scales [held][16], sums
   const int64_t n = g.n;
   const int C = (int)((n + kBlk - 1) / kBlk);
-  uint8_t *xs = lds + C * 2048;
+  const int held = C <= kStripBlocks ? C : kStripChunk;
+  uint8_t *xs = lds + held * 2048;
   const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int part = wave % kSplit;
@@ -782,8 +810,21 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(FewArgs g) {
   for (int u = 0; u < kRing; ++u)
     if (u < total) load(ring[u]);
 
-  // x, sixteen lanes a token and block
-  {
+  // x of the blocks first .. first + held - 1, rounded before: copied as it is,
+  // in pieces of 1 KiB
+  auto fetch = [&](int first) {
+    const int blocks = min(held, C - first);
+    for (int at = wave * 1024; at < blocks * 2048; at += kStripWaves * 1024)
+      copy16_from(g.xt.codes + first * 2048 + at + lane * 16, lds + at);
+    for (int at = wave * 1024; at < blocks * 16; at += kStripWaves * 1024)
+      if (at + lane * 16 < blocks * 16)
+        copy16_from(g.xt.codes + C * 2048 + first * 16 + at + lane * 16, xs + at);
+    step_barrier<0>();
+  };
+  if (g.xt.codes) {
+    fetch(0);
+  } else {
+    // sixteen lanes a token and block
     const typename D::raw *x = static_cast<const typename D::raw *>(g.x);
     const int k = threadIdx.x & 15;
     for (int piece = threadIdx.x >> 4; piece < g.T * C; piece += 4 * kStripWaves) {
@@ -795,13 +836,11 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(FewArgs g) {
 #pragma unroll
       for (int off = 8; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 16));
       const int e = block_exponent<kXFormat>(amax);
-      // columns 8 k .. belong to half k / 8, lane group (k / 2) mod 4
-      *reinterpret_cast<uint2 *>(lds + J * 2048 + (k >> 3) * 1024 + ((k >> 1 & 3) * 16 + t) * 16 +
-                                 (k & 1) * 8) = encode8<kXFormat>(v, pow2(-e));
+      *reinterpret_cast<uint2 *>(lds + operand_at(J, t, k)) = encode8<kXFormat>(v, pow2(-e));
       if (k == 0) xs[J * 16 + t] = (uint8_t)(e + 127);
     }
+    __syncthreads();
   }
-  __syncthreads();
 
   v4f acc = {};
   auto multiply = [&](const Block &b, int J) {
@@ -811,19 +850,7 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(FewArgs g) {
     const RowCodes x{*reinterpret_cast<const i32x4 *>(p), *reinterpret_cast<const i32x4 *>(p + 1024)};
     const int sx = xs[J * 16 + r];
     const v8i w = operand(RowCodes{b.lo, b.hi});
-    if constexpr (kOut == AF1_SRC_BF16) {
-      acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, operand(x), acc, kWFormat, kXFormat,
-                                                             0, b.sw, 0, sx);
-    } else {
-      bf8v a[4], c[4];
-      to_bf16<kWFormat>(w, a);
-      to_bf16<kXFormat>(operand(x), c);
-      v4f s = {};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[k], c[k], s, 0, 0, 0);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) acc[k] += ldexpf(s[k], b.sw + sx - 254);
-    }
+    acc = mul_block<kWFormat, kXFormat, kOut>(w, operand(x), acc, b.sw, sx);
   };
   auto store = [&](int strip, v4f v) {
     const int64_t row = (int64_t)strip * 16 + 4 * q;
@@ -858,12 +885,22 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(FewArgs g) {
     }
   } else {
     // one round: the launch has a workgroup for every kStrips strips
-    v4f *sums = reinterpret_cast<v4f *>(lds + ((C * 2064 + 15) & ~15));
-    for (int i = 0; i < total; i += kRing) {
+    v4f *sums = reinterpret_cast<v4f *>(lds + ((held * 2064 + 15) & ~15));
+    constexpr int kMine = kStripChunk / kSplit;  // blocks of a chunk, whole rings
+    static_assert(kMine % kRing == 0);
+    for (int first = 0; first < C; first += held) {
+      if (first > 0) {
+        __syncthreads();
+        fetch(first);
+      }
+      const int from = first == 0 ? 0 : first / kStripChunk * kMine;
+      const int to = held == C ? each : min(from + kMine, each);
+      for (int i = from; i < min(to, total); i += kRing) {
 #pragma unroll
-      for (int u = 0; u < kRing; ++u) {
-        if (i + u < total) multiply(ring[u], part + (i + u) * kSplit);
-        if (i + u + kRing < total) load(ring[u]);
+        for (int u = 0; u < kRing; ++u) {
+          if (i + u < total) multiply(ring[u], part + (i + u) * kSplit - first);
+          if (i + u + kRing < total) load(ring[u]);
+        }
       }
     }
     sums[wave * 64 + lane] = acc;
@@ -888,36 +925,106 @@ auto with_format(int f, F &&g) {
   return g(Int<AF1_FP8_E5M2>{});
 }
 
+constexpr int64_t kStripTokens = 16, kFewTokens = 32;
+constexpr int64_t kOwnPieces = 128;  // of x that a strip workgroup rounds itself
+
+// y = the partial sums' sum, in the ranges' order.
+template <typename D>
+__global__ __launch_bounds__(256) void sum_parts_kernel(const float *parts, int splits, int64_t n,
+                                                        typename D::raw *y) {
+  for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; 8 * c < n;
+       c += (int64_t)gridDim.x * 256) {
+    float s[8];
+    load8<F32>(parts, c, n, 0.f, s);
+    for (int k = 1; k < splits; ++k) {
+      float v[8];
+      load8<F32>(parts + k * n, c, n, 0.f, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] += v[i];
+    }
+    store8<D>(y, c, n, s);
+  }
+}
+
+unsigned grid_of(int64_t blocks) { return (unsigned)(blocks < (1 << 20) ? blocks : 1 << 20); }
+
 template <typename TT, int kWFormat, int kXFormat, int kOut>
-hipError_t launch_tiles(LinearArgs g, hipStream_t s) {
-  auto kernel = tile_kernel<TT, kWFormat, kXFormat, kOut>;
+hipError_t launch_tiles(LinearArgs g, int splits, float *parts, hipStream_t s) {
+  void *y = g.y;
   g.nW = (int)((g.m + TT::kTW - 1) / TT::kTW);
   g.nX = (int)((g.T + TT::kTX - 1) / TT::kTX);
-  kernel<<<(unsigned)g.nW * (unsigned)g.nX, TT::kThreads, TT::kLds, s>>>(g);
+  g.splits = splits;
+  if (splits > 1) g.y = parts;
+  tile_kernel<TT, kWFormat, kXFormat, kOut>
+      <<<(unsigned)(g.nW * g.nX * splits), TT::kThreads, TT::kLds, s>>>(g);
+  const hipError_t e = hipGetLastError();
+  if (splits == 1 || e != hipSuccess) return e;
+  const int64_t n = g.T * g.m;
+  const unsigned grid = (unsigned)((n + 2047) / 2048 < 4096 ? (n + 2047) / 2048 : 4096);
+  if constexpr (kOut == AF1_SRC_F32)
+    sum_parts_kernel<F32><<<grid, 256, 0, s>>>(parts, splits, n, static_cast<float *>(y));
+  else
+    sum_parts_kernel<BF16><<<grid, 256, 0, s>>>(parts, splits, n, static_cast<uint16_t *>(y));
   return hipGetLastError();
 }
 
-template <typename D, int kXFormat, int kWFormat, int kOut, int kFR, int kNT>
+// Which form computes T > 16 tokens, and over how many ranges of columns: the
+// least of the estimated times.  A tile takes `block` us a column block and
+// `fixed` us besides (first copies, epilogue) when every compute unit has one,
+// fitted to sweeps of T = 24 .. 2048 over eight shapes of 1024 x 4096 to 128256 x
+// 4096 (the choices were 1% above the best measured on average, 12% at most);
+// memory gives the weight at 5 TB/s at best; several ranges write and read
+// fp32 partial sums and take a launch more.
+enum Form { kFew, kTiles64, kTiles128, kTiles256 };
+struct Plan {
+  Form form;
+  int splits;
+};
+
+Plan plan_linear(int64_t m, int64_t n, int64_t T, int y_dtype) {
+  constexpr double kRate = 5e6;  // bytes a us
+  const bool f32 = y_dtype == AF1_SRC_F32;
+  const int64_t C = blocks_up(n), cus = device_cus();
+  const double weight = (double)m * n / kRate;
+  const auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+  Plan best{kTiles128, 1};
+  double least = 1e30;
+  const auto consider = [&](double us, Form f, int splits) {
+    us = us > weight ? us : weight;
+    if (splits > 1) us += 5 + 0.3 * splits + 8.0 * splits * T * m / kRate;
+    if (us < least) least = us, best = Plan{f, splits};
+  };
+  if (T <= kFewTokens) consider(up(up(m, 16), cus) * (2 + 1.2 * up(C, 8)), kFew, 1);
+  const struct {
+    Form form;
+    int rows, tokens;
+    double block, fixed;
+  } forms[] = {{kTiles64, 128, 64, f32 ? 0.73 : 0.55, f32 ? 4. : 3.},
+               {kTiles128, 128, 128, f32 ? 1.0 : 0.64, f32 ? 6. : 4.},
+               {kTiles256, 256, 256, 1.66, 6.}};
+  for (const auto &f : forms) {
+    if (f32 && f.form == kTiles256) continue;  // its sums would not leave registers for operands
+    const int64_t tiles = up(m, f.rows) * up(T, f.tokens);
+    for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
+      if (splits > 1 && C / splits < 4) break;
+      consider(up(tiles * splits, cus) * (up(C, splits) * f.block + f.fixed), f.form, splits);
+    }
+  }
+  return best;
+}
+
+template <int kXFormat, int kWFormat, int kOut>
 hipError_t launch_few(const FewArgs &g, hipStream_t s) {
-  constexpr int kWaves = 8;
-  constexpr int kLds = kWaves * kFR * kNT * 1024;
-  few_kernel<D, kXFormat, kWFormat, kOut, kFR, kNT, kWaves>
-      <<<(unsigned)((g.m + 16 * kFR - 1) / (16 * kFR)), 64 * kWaves, kLds, s>>>(g);
+  few_kernel<kXFormat, kWFormat, kOut><<<(unsigned)((g.m + 15) / 16), 64 * kFewWaves, 0, s>>>(g);
   return hipGetLastError();
-}
-
-// Strips a workgroup: more of them share an operand of x, fewer fill the device.
-template <typename D, int kXFormat, int kWFormat, int kOut, int kNT>
-hipError_t launch_few_rows(const FewArgs &g, hipStream_t s) {
-  if (g.m >= 64 * 512) return launch_few<D, kXFormat, kWFormat, kOut, kNT <= 2 ? 4 : 2, kNT>(g, s);
-  if (g.m >= 32 * 512) return launch_few<D, kXFormat, kWFormat, kOut, 2, kNT>(g, s);
-  return launch_few<D, kXFormat, kWFormat, kOut, 1, kNT>(g, s);
 }
 
 template <typename D, int kXFormat, int kWFormat, int kOut, int kSplit>
 hipError_t launch_strips(const FewArgs &g, hipStream_t s) {
-  const int64_t C = blocks_up(g.n), groups = (g.m + 16 * (kStripWaves / kSplit) - 1) / (16 * (kStripWaves / kSplit));
-  const size_t lds = ((C * 2064 + 15) & ~15) + (kSplit > 1 ? kStripWaves * 1024 : 0);
+  constexpr int kRows = 16 * (kStripWaves / kSplit);
+  const int64_t C = blocks_up(g.n), held = C <= kStripBlocks ? C : kStripChunk;
+  const int64_t groups = (g.m + kRows - 1) / kRows;
+  const size_t lds = ((held * 2064 + 15) & ~15) + (kSplit > 1 ? kStripWaves * 1024 : 0);
   const int64_t resident = device_cus() * (lds <= 80 * 1024 ? 2 : 1);
   const int64_t blocks = kSplit > 1 || groups < resident ? groups : resident;
   strip_kernel<D, kXFormat, kWFormat, kOut, kSplit><<<(unsigned)blocks, 64 * kStripWaves, lds, s>>>(g);
@@ -927,16 +1034,12 @@ hipError_t launch_strips(const FewArgs &g, hipStream_t s) {
 template <typename D, int kXFormat, int kWFormat, int kOut>
 hipError_t launch_strip_form(const FewArgs &g, hipStream_t s) {
   const int64_t strips = (g.m + 15) / 16, cus = device_cus();
-  if (strips >= 8 * cus) return launch_strips<D, kXFormat, kWFormat, kOut, 1>(g, s);
+  if (strips >= 8 * cus && blocks_up(g.n) <= kStripBlocks)
+    return launch_strips<D, kXFormat, kWFormat, kOut, 1>(g, s);
   if (strips >= 4 * cus) return launch_strips<D, kXFormat, kWFormat, kOut, 2>(g, s);
   if (strips >= 2 * cus) return launch_strips<D, kXFormat, kWFormat, kOut, 4>(g, s);
   return launch_strips<D, kXFormat, kWFormat, kOut, 8>(g, s);
 }
-
-unsigned grid_of(int64_t blocks) { return (unsigned)(blocks < (1 << 20) ? blocks : 1 << 20); }
-
-constexpr int64_t kStripBlocks = 72;  // as many as LDS holds
-constexpr int64_t kFewDense = 16, kFewTokens = 64;
 
 }  // namespace
 
@@ -972,9 +1075,15 @@ hipError_t launch_fp8_transpose(const af1_fp8_matrix &W, uint8_t *codes, uint8_t
   return hipGetLastError();
 }
 
-size_t fp8_linear_workspace_bytes(int64_t, int64_t n, int64_t T) {
-  if (T <= kFewDense) return 0;
-  return (size_t)blocks_up(T) * blocks_up(n) * (kTileBytes + kBlk);
+size_t fp8_linear_workspace_bytes(int64_t m, int64_t n, int64_t T) {
+  if (T <= kStripTokens)
+    return blocks_up(n) > kStripBlocks || T * blocks_up(n) > kOwnPieces ? blocks_up(n) * 2064 : 0;
+  int splits = 1;
+  for (int y : {AF1_SRC_F32, AF1_SRC_BF16}) {
+    const Plan p = plan_linear(m, n, T, y);
+    splits = p.splits > splits ? p.splits : splits;
+  }
+  return x_tile_bytes(n, T) + (splits > 1 ? (size_t)splits * T * m * 4 : 0);
 }
 
 template <int kXFormat, int kWFormat, int kOut>
@@ -983,29 +1092,44 @@ hipError_t launch_linear(const af1_fp8_matrix &W, const void *x, int x_dtype, in
   const int64_t m = W.rows, n = W.cols;
   const XTiles xt = x_tiles(ws, n, T);
   FewArgs few{W.codes, W.scales, x, xt, (int)T, m, n, y};
-  if (T <= kFewDense && blocks_up(n) <= kStripBlocks)
+  if (T <= kStripTokens) {
+    const bool own = T * blocks_up(n) <= kOwnPieces && blocks_up(n) <= kStripBlocks;
+    few.xt.codes = own ? nullptr : static_cast<uint8_t *>(ws);
     return with_type(x_dtype, [&](auto d) {
-      return launch_strip_form<decltype(d), kXFormat, kWFormat, kOut>(few, s);
+      using D = decltype(d);
+      if (!own) {
+        quantize_rows_kernel<D, kXFormat, true>
+            <<<(unsigned)((T * blocks_up(n) + 15) / 16), 256, 0, s>>>(
+                static_cast<const typename D::raw *>(x), T, n, few.xt);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+      }
+      return launch_strip_form<D, kXFormat, kWFormat, kOut>(few, s);
     });
-  if (T <= kFewDense)
-    return with_type(x_dtype, [&](auto d) {
-      return launch_few_rows<decltype(d), kXFormat, kWFormat, kOut, 1>(few, s);
-    });
+  }
   const hipError_t e = with_type(x_dtype, [&](auto d) {
     using D = decltype(d);
-    quantize_rows_kernel<D, kXFormat><<<grid_of((T * blocks_up(n) + 15) / 16), 256, 0, s>>>(
+    quantize_rows_kernel<D, kXFormat, false><<<grid_of((T * blocks_up(n) + 15) / 16), 256, 0, s>>>(
         static_cast<const typename D::raw *>(x), T, n, xt);
     return hipGetLastError();
   });
   if (e != hipSuccess) return e;
-  if (T <= 32) return launch_few_rows<F32, kXFormat, kWFormat, kOut, 2>(few, s);
-  if (T <= kFewTokens) return launch_few_rows<F32, kXFormat, kWFormat, kOut, 4>(few, s);
+  const Plan plan = plan_linear(m, n, T, kOut);
   LinearArgs g{W.codes, W.scales, xt, T, m, (int)blocks_up(n), (int)blocks_up(m),
-               (int)blocks_up(T), 0, 0, y};
-  if (kOut == AF1_SRC_F32 || T <= 1024)
-    return launch_tiles<Tile<128, 128, 2, 2, 4>, kWFormat, kXFormat, kOut>(g, s);
+               (int)blocks_up(T), 0, 0, 1, y};
+  float *parts = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + x_tile_bytes(n, T));
+  switch (plan.form) {
+    case kFew: return launch_few<kXFormat, kWFormat, kOut>(few, s);
+    case kTiles64:
+      return launch_tiles<Tile<128, 64, 2, 2, 8>, kWFormat, kXFormat, kOut>(g, plan.splits, parts, s);
+    case kTiles128:
+      return launch_tiles<Tile<128, 128, 2, 2, 4>, kWFormat, kXFormat, kOut>(g, plan.splits, parts, s);
+    default: break;
+  }
   if constexpr (kOut == AF1_SRC_BF16)
-    return launch_tiles<Tile<256, 256, 2, 2, 4>, kWFormat, kXFormat, kOut>(g, s);
+    return launch_tiles<Tile<256, 256, 2, 2, 4>, kWFormat, kXFormat, kOut>(g, plan.splits, parts, s);
+  else
+    return hipErrorInvalidValue;
 }
 
 hipError_t launch_fp8_linear(const af1_fp8_matrix &W, const void *x, int x_dtype, int x_format,
