@@ -83,19 +83,21 @@ __device__ __forceinline__ void rebase(Stat &s, float m, float c) {
   s.m = m;
 }
 
-// Eight logits, the largest of which is `top`.
-template <bool kEntropy>
-__device__ __forceinline__ void add8(Stat &s, const float (&x)[8], float top, float c) {
+// kN times eight logits, the largest of which is `top`.
+template <bool kEntropy, int kN>
+__device__ __forceinline__ void add(Stat &s, const float (&x)[kN][8], float top, float c) {
   rebase<kEntropy>(s, fmaxf(s.m, top), c);
   const float base = s.m == -kInf ? 0.f : s.m;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float t = (x[i] - base) * c;
-    const float e = exp2_hw(t);
-    s.Z += e;
-    // 2^-200 is 0 in fp32: masked entries add 0
-    if constexpr (kEntropy) s.W = fmaf(e, fmaxf(t, -200.f), s.W);
-  }
+  for (int n = 0; n < kN; ++n)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float t = (x[n][i] - base) * c;
+      const float e = exp2_hw(t);
+      s.Z += e;
+      // 2^-200 is 0 in fp32: masked entries add 0
+      if constexpr (kEntropy) s.W = fmaf(e, fmaxf(t, -200.f), s.W);
+    }
 }
 
 template <bool kEntropy>
@@ -192,38 +194,48 @@ struct Parts {
   int64_t size;
 };
 
-// The chunks of one part; calls f(chunk, x) for each of this thread's, whose
-// chunks lie kThreads apart, four loads in flight.
+// The chunks of one part; calls f(chunk, x) for this thread's, which lie
+// kThreads apart: two at a time (chunk and the next, x[2][8]) where there are
+// whole groups of four, with four loaded while four are worked on, and single
+// ones (x[1][8]) behind them.
 template <typename D, typename F>
 __device__ __forceinline__ void each_chunk(const typename D::raw *row, int64_t c0, int64_t c1,
                                            int64_t V, F &&f) {
-  constexpr int kAhead = 4;
-  const int64_t whole = min(c1, V / 8);
-  int64_t i = c0 + threadIdx.x;
-  for (; i + (kAhead - 1) * kThreads < whole; i += kAhead * kThreads) {
-    Eight<D> e[kAhead];
+  constexpr int kAhead = 4, kTurn = kAhead * kThreads;
+  const int whole = (int)min(c1, V / 8), end = (int)c1;
+  int i = (int)c0 + threadIdx.x;
+  Eight<D> e[kAhead];
+  const auto load = [&](int at) {
 #pragma unroll
-    for (int a = 0; a < kAhead; ++a) e[a] = load_raw<D>(row, i + a * kThreads);
+    for (int a = 0; a < kAhead; ++a) e[a] = load_raw<D>(row, at + a * kThreads);
+  };
+  if (i + (kAhead - 1) * kThreads < whole) load(i);
+  for (; i + (kAhead - 1) * kThreads < whole; i += kTurn) {
+    Eight<D> now[kAhead];
 #pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      float x[8];
-      widen<D>(e[a], x);
+    for (int a = 0; a < kAhead; ++a) now[a] = e[a];
+    if (i + kTurn + (kAhead - 1) * kThreads < whole) load(i + kTurn);
+#pragma unroll
+    for (int a = 0; a < kAhead; a += 2) {
+      float x[2][8];
+      widen<D>(now[a], x[0]);
+      widen<D>(now[a + 1], x[1]);
       f(i + a * kThreads, x);
     }
   }
-  for (; i < c1; i += kThreads) {
-    float x[8];
-    load8<D>(row, i, V, -kInf, x);
+  for (; i < end; i += kThreads) {
+    float x[1][8];
+    load8<D>(row, i, V, -kInf, x[0]);
     f(i, x);
   }
 }
 
 // ---------------------------------------------------------------------------
 // Alternatives.  Every thread remembers the first of its chunks that holds its
-// largest logit.  The k-th best of the threads' keys bounds the k-th best
-// logit from below, and only the threads at or above it, at most k, can hold
-// one of the best: their chunks are read again (from the caches), what reaches
-// the bound is collected and sorted.  Keys are distinct, so equal logits need
+// largest logit.  The k-th best of a wave's keys bounds the k-th best logit
+// from below, and so does the largest of the waves' bounds; only the threads at
+// or above it, at most k a wave, can hold one of the best: their chunks are
+// read again (from the caches), what reaches the bound is collected and sorted.  Keys are distinct, so equal logits need
 // no special case.  Rows with NaN, which the threads' largest logits do not
 // see, and rows with more to collect than there is room for are searched once
 // for every alternative.
@@ -232,10 +244,10 @@ __device__ __forceinline__ void each_chunk(const typename D::raw *row, int64_t c
 constexpr int kMaxFound = 512;  // collected logits; beyond it, one at a time
 
 struct TopLds {
-  uint64_t sorted[kWaves][64];
+  uint64_t waves[kWaves], scratch[64];
   uint64_t found[kMaxFound];
   uint64_t bound;
-  int holders[AF1_HEAD_MAX_TOP];
+  int holders[kWaves * AF1_HEAD_MAX_TOP];
   int n_holders, n_found;
 };
 
@@ -294,26 +306,14 @@ __device__ __forceinline__ uint64_t merge64(uint64_t a, const uint64_t *b) {
   return merge_steps<32>(max64(a, b[63 - (threadIdx.x & 63)]), true);
 }
 
-// In wave 0, lane i gets the i-th largest (i < 64) of the block's keys; the
-// other waves' value means nothing.
-__device__ __forceinline__ uint64_t block_sort(uint64_t v, TopLds &l) {
-  const int wave = threadIdx.x >> 6;
-  v = sort64(v);
-  l.sorted[wave][threadIdx.x & 63] = v;
-  __syncthreads();
-  if (wave == 0)
-    for (int w = 1; w < kWaves; ++w) v = merge64(v, l.sorted[w]);
-  return v;
-}
-
 // In wave 0, lane i gets the i-th largest of the n collected keys.
-__device__ __forceinline__ uint64_t sort_found(const TopLds &l, uint64_t *scratch) {
+__device__ __forceinline__ uint64_t sort_found(TopLds &l) {
   const int lane = threadIdx.x & 63, n = l.n_found;
   uint64_t v = sort64(lane < n ? l.found[lane] : 0);
   for (int at = 64; at < n; at += 64) {
-    scratch[lane] = sort64(at + lane < n ? l.found[at + lane] : 0);
+    l.scratch[lane] = sort64(at + lane < n ? l.found[at + lane] : 0);
     __builtin_amdgcn_wave_barrier();
-    v = merge64(v, scratch);
+    v = merge64(v, l.scratch);
     __builtin_amdgcn_wave_barrier();
   }
   return v;
@@ -335,9 +335,9 @@ __device__ __forceinline__ uint64_t one_by_one(int k, TopLds &l, F &&next) {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) b = max64(b, shfl_xor64(b, off));
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) l.sorted[0][threadIdx.x >> 6] = b;
+    if ((threadIdx.x & 63) == 0) l.waves[threadIdx.x >> 6] = b;
     __syncthreads();
-    for (int w = 0; w < kWaves; ++w) b = max64(b, l.sorted[0][w]);
+    for (int w = 0; w < kWaves; ++w) b = max64(b, l.waves[w]);
     if ((int)threadIdx.x == j) mine = b;
     last = b;
   }
@@ -351,11 +351,15 @@ template <typename D>
 __device__ uint64_t part_top(const typename D::raw *row, int64_t c0, int64_t c1, int64_t V, int k,
                              float best, int64_t chunk, bool odd, TopLds &l) {
   const uint64_t mine = chunk < 0 ? 0 : order_key(best, 8 * chunk + 7);
-  uint64_t v = block_sort(mine, l);
-  if (threadIdx.x == (unsigned)(k - 1)) l.bound = v;
+  const uint64_t v = sort64(mine);
+  if ((int)(threadIdx.x & 63) == k - 1) l.waves[threadIdx.x >> 6] = v;
   if (threadIdx.x == 0) l.n_holders = l.n_found = 0;
   __syncthreads();
-  if (mine != 0 && mine >= l.bound) l.holders[atomicAdd(&l.n_holders, 1)] = threadIdx.x;
+  uint64_t bound = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) bound = max64(bound, l.waves[w]);
+  if (threadIdx.x == 0) l.bound = bound;
+  if (mine != 0 && mine >= bound) l.holders[atomicAdd(&l.n_holders, 1)] = threadIdx.x;
   __syncthreads();
   const int64_t each = (c1 - c0 + kThreads - 1) / kThreads;
   for (int64_t i = threadIdx.x; i < l.n_holders * each; i += kThreads) {
@@ -377,7 +381,7 @@ __device__ uint64_t part_top(const typename D::raw *row, int64_t c0, int64_t c1,
       }
       return b;
     });
-  return threadIdx.x < 64 ? sort_found(l, l.sorted[1]) : 0;
+  return threadIdx.x < 64 ? sort_found(l) : 0;
 }
 
 template <typename D>
@@ -408,12 +412,18 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const typename D::ra
   const int64_t c0 = part * parts.size, c1 = min(c0 + parts.size, (V + 7) / 8);
   Stat s = no_logits();
   float best = -kInf;
-  int64_t chunk = -1;
-  each_chunk<D>(row, c0, c1, V, [&](int64_t i, const float(&x)[8]) {
-    const float m = max8(x);
-    if constexpr (kTop)
-      if (chunk < 0 || m > best) best = m, chunk = i;
-    add8<true>(s, x, m, c);
+  int chunk = -1;
+  each_chunk<D>(row, c0, c1, V, [&](int i, const auto &x) {
+    constexpr int kN = sizeof(x) / 32;
+    float top = -kInf;
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+      const float m = max8(x[n]);
+      if constexpr (kTop)
+        if (chunk < 0 || m > best) best = m, chunk = i + n * kThreads;
+      top = fmaxf(top, m);
+    }
+    add<true>(s, x, top, c);
   });
   s = block_join<true>(s, c, sh);
   uint64_t key = 0;
@@ -465,7 +475,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(const typename 
         return b;
       });
     else
-      key = threadIdx.x < 64 ? sort_found(l, l.sorted[1]) : 0;
+      key = threadIdx.x < 64 ? sort_found(l) : 0;
     write_top<D>(o, row, r, s, key);
   }
 }
@@ -490,20 +500,24 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(
   }
   if (y >= V) gl = __builtin_nanf("");
   const float c = scale * kLog2e;
-  each_chunk<D>(z + r * ld, c0, c1, V, [&](int64_t i, const float(&x)[8]) {
-    float d[8];
+  each_chunk<D>(z + r * ld, c0, c1, V, [&](int first, const auto &x) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float t = fmaf(x[j] - sv.x, c, -sv.w);  // log2 of the probability
-      const float p = exp2_hw(t);
-      d[j] = p == 0.f ? 0.f : -p * fmaf(gh, fmaf(kLn2, t, sv.z), gl);
-    }
-    if (y >= 8 * i && y < 8 * i + 8) {
+    for (int n = 0; n < (int)(sizeof(x) / 32); ++n) {
+      const int64_t i = first + n * kThreads;
+      float d[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (8 * i + j == y) d[j] += gl;
+      for (int j = 0; j < 8; ++j) {
+        const float t = fmaf(x[n][j] - sv.x, c, -sv.w);  // log2 of the probability
+        const float p = exp2_hw(t);
+        d[j] = p == 0.f ? 0.f : -p * fmaf(gh, fmaf(kLn2, t, sv.z), gl);
+      }
+      if (y >= 8 * i && y < 8 * i + 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (8 * i + j == y) d[j] += gl;
+      }
+      store8<D>(out, i, V, d);
     }
-    store8<D>(out, i, V, d);
   });
 }
 
@@ -578,11 +592,11 @@ __device__ __forceinline__ void part_stats(const typename D::raw *s, const typen
                                            Stat &a, Stat &b) {
   a = b = no_logits();
   for (int64_t i = c0 + threadIdx.x; i < c1; i += kThreads) {
-    float x[8], w[8];
-    load8<D>(s, i, V, -kInf, x);
-    load8<D>(t, i, V, -kInf, w);
-    add8<false>(a, x, max8(x), c);
-    add8<false>(b, w, max8(w), c);
+    float x[1][8], w[1][8];
+    load8<D>(s, i, V, -kInf, x[0]);
+    load8<D>(t, i, V, -kInf, w[0]);
+    add<false>(a, x, max8(x[0]), c);
+    add<false>(b, w, max8(w[0]), c);
   }
   __syncthreads();
   a = block_join<false>(a, c, l.wave);
@@ -692,11 +706,11 @@ __global__ __launch_bounds__(kThreads, 4) void kl_kernel(const typename D::raw *
 #pragma unroll
   for (int j = 0; j < kChunks; ++j) {
     if (c0 + j * kThreads >= c1) break;
-    float x[8];
-    widen<D>(xs[j], x);
-    add8<false>(a, x, max8(x), c);
-    widen<D>(xt[j], x);
-    add8<false>(b, x, max8(x), c);
+    float x[1][8];
+    widen<D>(xs[j], x[0]);
+    add<false>(a, x, max8(x[0]), c);
+    widen<D>(xt[j], x[0]);
+    add<false>(b, x, max8(x[0]), c);
   }
   a = block_join<false>(a, c, l.wave);
   b = block_join<false>(b, c, l.wave + kWaves);
