@@ -18,9 +18,12 @@ LIB = os.path.join(HERE, "libaf1.so")
 NABF_LIB = os.path.join(HERE, "libaf1_nabf.so")
 HEAD_LIB = os.path.join(HERE, "libaf1_head.so")
 HEAD_SRCS = ("af1_head_api.hip", "af1_fp8.hip", "af1_logits.hip")
-# libaf1.so with -DAF1_TEST_BUILD: tests only, nothing else loads it
+# libaf1.so and libaf1_head.so with -DAF1_TEST_BUILD: tests only, nothing else
+# loads them
 TEST_LIB = os.path.join(HERE, "libaf1_test.so")
-TEST_SRCS = ("af1_gemv.hip", "af1_gemm.hip")  # the sources that it compiles differently
+HEAD_TEST_LIB = os.path.join(HERE, "libaf1_head_test.so")
+# the sources that they compile differently
+TEST_SRCS = ("af1_gemv.hip", "af1_gemm.hip", "af1_fp8.hip", "af1_logits.hip")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
@@ -57,10 +60,10 @@ def _link(out: str, objs, libs, verbose: bool) -> None:
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every source; link libaf1.so (the layer), its test build
-    libaf1_test.so, libaf1_nabf.so (the offline NABF building blocks, which
-    also need rocBLAS and rocSOLVER and reuse the sign-packing kernel) and
-    libaf1_head.so (the output head).  Returns the path of libaf1.so."""
+    """Compile every source; link libaf1.so (the layer), libaf1_nabf.so (the
+    offline NABF building blocks, which also need rocBLAS and rocSOLVER and reuse
+    the sign-packing kernel), libaf1_head.so (the output head), and the test
+    builds of the first and the last.  Returns the path of libaf1.so."""
     os.makedirs(BUILD, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
     with cf.ThreadPoolExecutor(max_workers=8) as ex:
@@ -72,8 +75,9 @@ def build(verbose: bool = False) -> str:
     head_srcs = [os.path.join(CSRC, s) for s in HEAD_SRCS]
     layer = [s for s in objs if s != nabf_src and s not in head_srcs]
     _link(LIB, [objs[s] for s in layer], [], verbose)
-    _link(TEST_LIB, [tests[s].result() if s in tests else objs[s] for s in layer], [], verbose)
     _link(HEAD_LIB, [objs[s] for s in head_srcs], [], verbose)
+    for out, part in ((TEST_LIB, layer), (HEAD_TEST_LIB, head_srcs)):
+        _link(out, [tests[s].result() if s in tests else objs[s] for s in part], [], verbose)
     _link(NABF_LIB, [objs[nabf_src], objs[pack_src]],
           ["-L/opt/rocm/lib", "-lrocsolver", "-lrocblas"], verbose)
     return LIB

@@ -1144,3 +1144,14 @@ hipError_t launch_fp8_linear(const af1_fp8_matrix &W, const void *x, int x_dtype
 }
 
 }  // namespace af1h
+
+#ifdef AF1_TEST_BUILD
+// The form of a linear's T > 16 tokens (a Form) and its ranges of columns.
+extern "C" AF1_API int af1_test_linear_plan(int64_t m, int64_t n, int64_t T, int32_t y_dtype,
+                                            int32_t *out) {
+  const af1h::Plan p = af1h::plan_linear(m, n, T, y_dtype);
+  out[0] = p.form;
+  out[1] = p.splits;
+  return 0;
+}
+#endif
