@@ -238,21 +238,23 @@ def token_logprobs(logits, targets=None, k=0, scale=1.0, ws=None, stream=None):
 def _logprobs_call(logits, rows, targets, k, scale, ws, stream):
     dtype, T, V, ld = rows
     dev = logits.device
-    # the saved rows first: they are 16 bytes each and aligned so
-    saved, entropy, lse, logprob, top = torch.empty(
-        (7 + k) * T, dtype=torch.float32, device=dev).split((4 * T, T, T, T, k * T))
-    saved, index = saved.view(T, 4), None
+    need = head.af1_token_logprobs_workspace_bytes(T, V, k) if ws is None else 0
+    # one block: the saved rows and the workspace first, which are aligned to 16
+    # bytes, then what belongs to tokens
+    saved, own, entropy, lse, logprob, top = torch.empty(
+        (7 + k) * T + need // 4, dtype=torch.float32, device=dev).split(
+            (4 * T, need // 4, T, T, T, k * T))
+    index = None
     if targets is None:
         logprob = None
     if k:
         top, index = top.view(T, k), torch.empty((T, k), dtype=torch.int64, device=dev)
     else:
         top = None
-    ws, size = _workspace(ws, head.af1_token_logprobs_workspace_bytes(T, V, k)
-                          if ws is None else 0, dev)
+    ws, size = (own, need) if ws is None else _workspace(ws, 0, dev)
     head.af1_token_logprobs(logits, dtype, T, V, ld, scale, targets, logprob, entropy, lse, k, top,
                             index, saved, ws, size, stream)
-    return TokenLogprobs(logprob, entropy, lse, top, index, saved)
+    return TokenLogprobs(logprob, entropy, lse, top, index, saved.view(T, 4))
 
 
 def token_logprobs_backward(logits, targets, result, g_logprob=None, g_entropy=None, scale=1.0,
