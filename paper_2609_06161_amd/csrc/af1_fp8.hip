@@ -293,7 +293,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 // The first `left` (or all) of eight values.
 __device__ __forceinline__ void store8_bf16(uint16_t *p, int64_t left, uint4 v) {
   if (left >= 8) {
-    *reinterpret_cast<Chunk *>(p) = Chunk{{v.x, v.y, v.z, v.w}};
+    typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+    __builtin_nontemporal_store(u4{v.x, v.y, v.z, v.w}, reinterpret_cast<u4 *>(p));
     return;
   }
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
