@@ -27,6 +27,7 @@ typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
 
 constexpr int64_t kTileBytes = kBlk * kBlk;
+constexpr int kHalfBytes = kBlk * 64;  // 64 columns of a tile of tokens
 
 // |x| of a finite entry, 0 for the others: what a block's scale is chosen from.
 __device__ __forceinline__ float finite_abs(float x) {
@@ -232,7 +233,8 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const typename D::ra
     }
     const int64_t tile = t / kBlk * C + J;
     const int row = (int)(t % kBlk);
-    *reinterpret_cast<uint2 *>(out.codes + tile * kTileBytes + row * kBlk + k * 8) = codes;
+    *reinterpret_cast<uint2 *>(out.codes + tile * kTileBytes + (k >> 3) * kHalfBytes + row * 64 +
+                               (k & 7) * 8) = codes;
     if (k == 0) out.scales[tile * kBlk + (row & 31) * 4 + (row >> 5)] = (uint8_t)(e + 127);
   }
 }
@@ -415,6 +417,7 @@ __global__ __launch_bounds__(TT::kThreads, TT::kResident) void tile_kernel(Linea
   const i32x4 wr = make_rsrc(g.wcodes + wb0 * band);
   const i32x4 xr = make_rsrc(g.x.codes + xb0 * band);
   const int voff = (lane >> 2) * kBlk + (((lane & 3) ^ (lane >> 4)) << 4);
+  const int voffx = (lane >> 2) * 64 + (((lane & 3) ^ (lane >> 4)) << 4);
   int soff[TT::kCopies];
 #pragma unroll
   for (int q = 0; q < TT::kCopies; ++q) {
@@ -424,7 +427,7 @@ __global__ __launch_bounds__(TT::kThreads, TT::kResident) void tile_kernel(Linea
     // a tile may reach past the last block: it reads that one again, and what
     // comes of it is not stored
     const int blk = min(at >> 7, (isw ? g.R - 1 - wb0 : g.X - 1 - xb0));
-    soff[q] = (int)(blk * band) + (at & 127) * kBlk;
+    soff[q] = (int)(blk * band) + (at & 127) * (isw ? kBlk : 64);
   }
   // operands: rows row0 .. of W and tokens tok0 .. of the tile
   const int row0 = wave / TT::kWC * kFR * 32, tok0 = wave % TT::kWC * kFC * 32;
@@ -438,8 +441,9 @@ __global__ __launch_bounds__(TT::kThreads, TT::kResident) void tile_kernel(Linea
     uint8_t *st = lds + (s & (kS - 1)) * TT::kStage;
     const int J = J0 + (s >> 1), p = wave * TT::kCopies + k;
     if (k < TT::kCopies)
-      copy16(16 * p < TT::kTW ? wr : xr, st + p * 1024, voff,
-             soff[k < TT::kCopies ? k : 0] + J * (int)kTileBytes + (s & 1) * 64);
+      copy16(16 * p < TT::kTW ? wr : xr, st + p * 1024, 16 * p < TT::kTW ? voff : voffx,
+             soff[k < TT::kCopies ? k : 0] + J * (int)kTileBytes +
+                 (s & 1) * (16 * p < TT::kTW ? 64 : kHalfBytes));
     else if (k == TT::kCopies)
       copy4(xsc + J * kBlk, st + TT::kCodes + wave * 512);
     else
@@ -700,7 +704,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewArgs g) {
   const int64_t row0 = (int64_t)blockIdx.x * 16;
   const uint8_t *w = g.wcodes + row0 / kBlk * C * kTileBytes + (row0 % kBlk + r) * kBlk + q * 16;
   const uint8_t *wsc = g.wscales + row0 / kBlk * C;
-  const uint8_t *x = g.xt.codes + r * kBlk + q * 16, *xsc = g.xt.scales + r * 4;
+  const uint8_t *x = g.xt.codes + r * 64 + q * 16, *xsc = g.xt.scales + r * 4;
 
   struct Block {
     RowCodes w, x[2];
@@ -712,8 +716,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewArgs g) {
     b.sw = wsc[J];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      p = reinterpret_cast<const i32x4 *>(x + J * kTileBytes + t * 16 * kBlk);
-      b.x[t] = RowCodes{p[0], p[4]};
+      const uint8_t *xt = x + J * kTileBytes + t * 16 * 64;
+      b.x[t] = RowCodes{*reinterpret_cast<const i32x4 *>(xt),
+                        *reinterpret_cast<const i32x4 *>(xt + kHalfBytes)};
       b.sx[t] = xsc[J * kBlk + t * 64];
     }
   };
