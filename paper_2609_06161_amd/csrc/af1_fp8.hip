@@ -308,23 +308,35 @@ __device__ __forceinline__ void store8_bf16(uint16_t *p, int64_t left, uint4 v) 
 // ---------------------------------------------------------------------------
 // Tiled product.  A workgroup of kWR x kWC waves computes kTW rows of W x kTX
 // tokens; a wave kFR x kFC pieces of 32 x 32.  A step is half a column block
-// (64 columns).  Its bytes go from memory straight into one of kStages LDS
-// buffers (buffer loads with an LDS destination) and from there into registers
-// one step before they are multiplied, so in step s
-//   buffer s + 1 has landed and is read into registers,
-//   buffers s + 2 .. s + kStages - 1 are on their way, and
-//   buffer s, whose operands are in registers, is filled with step s + kStages.
-// A step meets the other waves once; nothing in it waits for memory that was
-// asked for in the last kStages - 2 steps.  (With two buffers of a whole block
-// each, which hold as many bytes, a step waited for copies issued in the step
-// before: 1289 us where this takes 992 at 128256 x 4096 and 2048 tokens.)
+// (64 columns).  Codes go from memory straight into LDS (buffer loads with an
+// LDS destination) and from there into registers one step before they are
+// multiplied.  The 256 x 256 tile keeps three blocks of W and three steps of
+// tokens in LDS, so in step s = 2 J + h
+//   the operands of s are in registers, those of s + 1 are read,
+//   the tokens of s + 3 and half of the rows of W's block J + 2 (h = 0) or J + 3
+//   (h = 1) are asked for, and
+//   what was asked for one step ago, and W's half of two steps ago, may be on
+//   its way.
+// The smaller tiles keep four steps of both and ask for step s + 4: as many bytes,
+// but more of them in flight, and two workgroups fit a compute unit (500 tokens of
+// 8192 x 8192: 43.7 us, by blocks 44.6).  A step meets the other waves once.
 //
-// LDS holds rows of 64 bytes, four chunks of 16.  A copy instruction writes 64
-// consecutive chunks (sixteen rows), one a lane, and a lane chooses its
-// source: chunk c of row r is kept at position c XOR (r / 4 mod 4).  The LDS
-// serves a 16-byte read of 64 lanes in groups of sixteen, of which four have
-// equal r mod 4; these then fall in distinct banks (counted: 0.3 conflict
-// cycles a read, against 4.1 with rows of 128 bytes and c XOR (r mod 8)).
+// What bounds the large tile is the L2's request rate: 64 KiB a block and tile in
+// requests of 128 bytes where a copy covers whole lines, else twice as many.  That
+// is why W, whose tiles have rows of 128 columns, is copied by blocks there, and
+// why the tokens' codes in the workspace are laid out by halves.  Measured at
+// 128256 x 4096 and 2048 tokens: two buffers of a whole block, copied in a burst,
+// 1289 us; four of half blocks with the copies between the products 1019; the
+// tokens by whole lines 962; W too 922.  (A workgroup that takes tile after tile
+// and stores one under the next one's first copies took 955: what its steps need
+// besides in scalar instructions costs more than the overlap gives.)
+//
+// LDS rows of 128 bytes (W's block) have eight chunks of 16; chunk c of row r is
+// kept at position c XOR (r / 2 mod 8).  Rows of 64 bytes have chunk c at c XOR (r
+// / 4 mod 4).  A copy instruction writes 64 consecutive chunks, one a lane, and a
+// lane chooses its source.  The LDS serves a 16-byte read of 64 lanes in groups of
+// sixteen, not of consecutive rows but with two of each r / 2 mod 8 (four of each
+// r mod 4); these then fall in distinct banks.
 // ---------------------------------------------------------------------------
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -334,28 +346,38 @@ __device__ __forceinline__ i32x4 make_rsrc(const void *p) {
   return i32x4{(int)(uint32_t)a, (int)(uint32_t)(a >> 32), 0x7fffffff, 0x00020000};
 }
 
+// The same memory, or with !live none of it: a copy from there, at offset 0,
+// asks memory for nothing.
+__device__ __forceinline__ i32x4 only_if(i32x4 r, bool live) {
+  r[2] = live ? r[2] : 0;
+  return r;
+}
+
+// A copy waits for M0 as long as the compiler would have its own instructions.
+
 // One 16-byte chunk a lane from rsrc + voff + soff into 64 chunks at dst.
 __device__ __forceinline__ void copy16(i32x4 r, uint8_t *dst, int voff, int soff) {
   const uint32_t m = (uint32_t)(size_t)(lds_void *)dst;
-  asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(voff), "s"(r), "s"(soff), "{m0}"(m)
+  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(voff), "s"(r),
+               "s"(soff), "{m0}"(m)
                : "memory");
 }
 
 // 16 bytes a lane from the lane's own address into 64 chunks at dst.
 __device__ __forceinline__ void copy16_from(const void *src, uint8_t *dst) {
   const uint32_t m = (uint32_t)(size_t)(lds_void *)dst;
-  asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(m) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(m) : "memory");
 }
 
 // One dword, or one byte, a lane from the lane's own address into 64 dwords at
 // dst.
 __device__ __forceinline__ void copy4(const void *src, uint8_t *dst) {
   const uint32_t m = (uint32_t)(size_t)(lds_void *)dst;
-  asm volatile("global_load_lds_dword %0, off" ::"v"(src), "{m0}"(m) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "{m0}"(m) : "memory");
 }
 __device__ __forceinline__ void copy1(const void *src, uint8_t *dst) {
   const uint32_t m = (uint32_t)(size_t)(lds_void *)dst;
-  asm volatile("global_load_lds_ubyte %0, off" ::"v"(src), "{m0}"(m) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_ubyte %0, off" ::"v"(src), "{m0}"(m) : "memory");
 }
 
 // All but kLeft of this wave's copies have landed, its LDS reads are done, and
@@ -366,21 +388,28 @@ __device__ __forceinline__ void step_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLeft) : "memory");
 }
 
-template <int kTW_, int kTX_, int kWR_, int kWC_, int kStages_>
+template <int kTW_, int kTX_, int kWR_, int kWC_>
 struct Tile {
-  static constexpr int kTW = kTW_, kTX = kTX_, kWR = kWR_, kWC = kWC_, kStages = kStages_;
+  static constexpr int kTW = kTW_, kTX = kTX_, kWR = kWR_, kWC = kWC_;
   static constexpr int kWaves = kWR * kWC, kThreads = 64 * kWaves;
   static constexpr int kFR = kTW / kWR / 32, kFC = kTX / kWC / 32;  // pieces a wave
-  static constexpr int kCodes = (kTW + kTX) * 64;      // LDS bytes a step
-  static constexpr int kStage = kCodes + kWaves * 512;  // and the scales', two slots a wave
-  static constexpr int kCopies = kCodes / 1024 / kWaves;  // a wave and step, and two of scales
+  static constexpr bool kBlocks = kTW * kTX > 128 * 128;  // W is copied by blocks
+  // LDS: a ring of W's blocks or halves, of the tokens' steps and of scales
+  static constexpr int kSlots = kBlocks ? 3 : 4;
+  static constexpr int kWSlot = kTW * (kBlocks ? 128 : 64), kXSlot = kTX * 64;
+  static constexpr int kSSlot = kWaves * 512;
+  static constexpr int kXAt = kSlots * kWSlot, kSAt = kXAt + kSlots * kXSlot;
+  static constexpr int kRing = kSAt + kSlots * kSSlot;
+  // a wave's copies in a step: half of W's block, the tokens', two of scales
+  static constexpr int kWCopies = kTW * 64 / 1024 / kWaves, kXCopies = kXSlot / 1024 / kWaves;
+  static constexpr int kCopies = kWCopies + kXCopies + 2;
   static constexpr int kOutRow = kFR * 64 + 16;  // LDS bytes of a token's bf16 outputs
   static constexpr int kOutLds = kWaves * 32 * kOutRow;
   // waves a SIMD that the registers have to leave room for
   static constexpr int kResident = kTW * kTX > 128 * 128 ? 1 : 2;
-  static constexpr int kLds = kStages * kStage > kOutLds ? kStages * kStage : kOutLds;
-  static_assert(kCodes % (1024 * kWaves) == 0 && kTW % 16 == 0 && kTX % 16 == 0);
-  static_assert((kStages & (kStages - 1)) == 0 && kLds <= 160 * 1024);
+  static constexpr int kLds = kRing > kOutLds ? kRing : kOutLds;
+  static_assert(kWCopies >= 1 && kWCopies * 1024 * kWaves == kTW * 64 && kWCopies % 2 == 0);
+  static_assert(kXCopies >= 1 && kXCopies * 1024 * kWaves == kXSlot && kLds <= 160 * 1024);
 };
 
 struct LinearArgs {
@@ -396,7 +425,7 @@ struct LinearArgs {
 
 template <typename TT, int kWFormat, int kXFormat, int kOut>
 __global__ __launch_bounds__(TT::kThreads, TT::kResident) void tile_kernel(LinearArgs g) {
-  constexpr int kFR = TT::kFR, kFC = TT::kFC, kS = TT::kStages;
+  constexpr int kFR = TT::kFR, kFC = TT::kFC;
   extern __shared__ uint8_t lds[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
@@ -411,43 +440,59 @@ __global__ __launch_bounds__(TT::kThreads, TT::kResident) void tile_kernel(Linea
   // this range's blocks
   const int J0 = (int)((int64_t)C * part / g.splits), J1 = (int)((int64_t)C * (part + 1) / g.splits);
 
-  // copy roles: piece p = wave kCopies + q is sixteen tile rows, W's first
+  // copy roles: W's piece p = wave 2 kWCopies + q is eight rows of a block, the
+  // tokens' piece wave kXCopies + q sixteen rows of a step
   const int64_t band = (int64_t)C * kTileBytes;  // bytes of 128 rows
   const int wb0 = w0 >> 7, xb0 = x0 >> 7;
   const i32x4 wr = make_rsrc(g.wcodes + wb0 * band);
   const i32x4 xr = make_rsrc(g.x.codes + xb0 * band);
-  const int voff = (lane >> 2) * kBlk + (((lane & 3) ^ (lane >> 4)) << 4);
-  const int voffx = (lane >> 2) * 64 + (((lane & 3) ^ (lane >> 4)) << 4);
-  int soff[TT::kCopies];
-#pragma unroll
-  for (int q = 0; q < TT::kCopies; ++q) {
-    const int row = 16 * (wave * TT::kCopies + q);
-    const bool isw = row < TT::kTW;
-    const int at = isw ? (w0 & 127) + row : (x0 & 127) + row - TT::kTW;
-    // a tile may reach past the last block: it reads that one again, and what
-    // comes of it is not stored
-    const int blk = min(at >> 7, (isw ? g.R - 1 - wb0 : g.X - 1 - xb0));
-    soff[q] = (int)(blk * band) + (at & 127) * (isw ? kBlk : 64);
-  }
+  // a lane's chunk of a piece: of eight rows of a block of W (row lane / 8, which
+  // is row 4 (p mod 2) + .. of eight pairs), or of sixteen half rows
+  const int wv0 = TT::kBlocks ? (lane >> 3) * kBlk + (((lane & 7) ^ (lane >> 4)) << 4)
+                              : (lane >> 2) * kBlk + (((lane & 3) ^ (lane >> 4)) << 4);
+  const int wv1 = TT::kBlocks ? wv0 ^ (4 << 4) : wv0;
+  const int xv = (lane >> 2) * 64 + (((lane & 3) ^ (lane >> 4)) << 4);
+  // A wave copies rows of one 128-row block.  A tile may reach past the last
+  // block: it reads that one again, and what comes of it is not stored.
+  const int wat = (w0 & 127) + wave * (TT::kTW / TT::kWaves);
+  const int xat = (x0 & 127) + wave * (TT::kTX / TT::kWaves);
+  static_assert(128 % (TT::kTW / TT::kWaves) == 0 && 128 % (TT::kTX / TT::kWaves) == 0);
+  const int woff = (int)(min(wat >> 7, g.R - 1 - wb0) * band) + (wat & 127) * kBlk +
+                   J0 * (int)kTileBytes;
+  const int xoff = (int)(min(xat >> 7, g.X - 1 - xb0) * band) + (xat & 127) * 64 +
+                   J0 * (int)kTileBytes;
   // operands: rows row0 .. of W and tokens tok0 .. of the tile
   const int row0 = wave / TT::kWC * kFR * 32, tok0 = wave % TT::kWC * kFC * 32;
   const int wblk = min((w0 + row0) >> 7, g.R - 1), xblk = min((x0 + tok0) >> 7, g.X - 1);
   // scales: the tokens' dwords and W's byte of a block, each lane its own
-  const uint8_t *wsc = g.wscales + (int64_t)wblk * C;
-  const uint8_t *xsc = g.x.scales + (int64_t)xblk * C * kBlk + r * 4;
-  // copy k of step s: codes, then the scales
-  constexpr int kCopies = TT::kCopies + 2;
-  auto copy = [&](int s, int k) {
-    uint8_t *st = lds + (s & (kS - 1)) * TT::kStage;
-    const int J = J0 + (s >> 1), p = wave * TT::kCopies + k;
-    if (k < TT::kCopies)
-      copy16(16 * p < TT::kTW ? wr : xr, st + p * 1024, 16 * p < TT::kTW ? voff : voffx,
-             soff[k < TT::kCopies ? k : 0] + J * (int)kTileBytes +
-                 (s & 1) * (16 * p < TT::kTW ? 64 : kHalfBytes));
-    else if (k == TT::kCopies)
-      copy4(xsc + J * kBlk, st + TT::kCodes + wave * 512);
+  const uint8_t *wsc = g.wscales + (int64_t)wblk * C + J0;
+  const uint8_t *xsc = g.x.scales + ((int64_t)xblk * C + J0) * kBlk + r * 4;
+  // Blocks behind the range's last one are asked for too, of no memory, so that
+  // the steps are all alike: a branch around a copy or a last step of its own
+  // would move the accumulators between registers.
+  const int blocks = J1 - J0;
+  // copy k of half q of W's block J into ring slot `slot`: of half the wave's rows,
+  // or of half the columns
+  auto copy_w = [&](int slot, int J, int q, int k) {
+    const bool live = J < blocks;
+    const int p = TT::kBlocks ? (wave * 2 + q) * TT::kWCopies + k : wave * TT::kWCopies + k;
+    const int from = TT::kBlocks ? (q * TT::kWCopies + k) * 1024 : k * 2048 + q * 64;
+    copy16(only_if(wr, live), lds + slot * TT::kWSlot + p * 1024, k & 1 ? wv1 : wv0,
+           live ? woff + J * (int)kTileBytes + from : 0);
+  };
+  // the scales (k = 0, 1) and the tokens of step s
+  auto copy_x = [&](int slot, int s, int k) {
+    const int J = s >> 1;
+    const bool live = J < blocks;
+    uint8_t *sc = lds + TT::kSAt + slot * TT::kSSlot + wave * 512;
+    if (k == 0)
+      copy4(xsc + min(J, blocks - 1) * kBlk, sc);
+    else if (k == 1)
+      copy1(wsc + min(J, blocks - 1), sc + 256);
     else
-      copy1(wsc + J, st + TT::kCodes + wave * 512 + 256);
+      copy16(only_if(xr, live),
+             lds + TT::kXAt + slot * TT::kXSlot + (wave * TT::kXCopies + k - 2) * 1024, xv,
+             live ? xoff + J * (int)kTileBytes + (s & 1) * kHalfBytes + (k - 2) * 1024 : 0);
   };
 
   const int xshift = 8 * (((x0 + tok0) & 127) >> 5);
@@ -455,23 +500,25 @@ __global__ __launch_bounds__(TT::kThreads, TT::kResident) void tile_kernel(Linea
     v8i a[kFR], b[kFC];
     int sw, sx;
   };
-  // piece k of step s: W's, the tokens', the scales
+  // piece k of a step: the scales, W's rows (half `half` of a block), the tokens
   constexpr int kReads = kFR + kFC + 1;
-  const int lo = ((2 * h) ^ (r >> 2 & 3)) << 4, hi = lo ^ 16;
-  auto read = [&](int s, int k, Operands &o) {
-    const uint8_t *st = lds + (s & (kS - 1)) * TT::kStage;
+  const int xlo = ((2 * h) ^ (r >> 2 & 3)) << 4, wlo = ((2 * h) ^ (r >> 1 & 7)) << 4;
+  auto read = [&](int wslot, int xslot, int half, int k, Operands &o) {
     if (k == 0) {
-      const uint32_t *sc = reinterpret_cast<const uint32_t *>(st + TT::kCodes + wave * 512);
+      const uint32_t *sc =
+          reinterpret_cast<const uint32_t *>(lds + TT::kSAt + xslot * TT::kSSlot + wave * 512);
       o.sx = (int)(sc[r] >> xshift);
       o.sw = (int)sc[64 + lane];
       return;
     }
-    const int piece = k - 1;
-    const int row = piece < kFR ? row0 + 32 * piece : TT::kTW + tok0 + 32 * (piece - kFR);
-    const uint8_t *p = st + (row + r) * 64;
+    const int i = k - 1, j = i - kFR;
+    constexpr int kWRow = TT::kBlocks ? 128 : 64;
+    const uint8_t *p = i < kFR ? lds + wslot * TT::kWSlot + (row0 + 32 * i + r) * kWRow
+                               : lds + TT::kXAt + xslot * TT::kXSlot + (tok0 + 32 * j + r) * 64;
+    const int lo = i < kFR && TT::kBlocks ? wlo ^ (half << 6) : xlo;
     const i32x4 u = *reinterpret_cast<const i32x4 *>(p + lo);
-    const i32x4 v = *reinterpret_cast<const i32x4 *>(p + hi);
-    (piece < kFR ? o.a[piece < kFR ? piece : 0] : o.b[piece < kFR ? 0 : piece - kFR]) =
+    const i32x4 v = *reinterpret_cast<const i32x4 *>(p + (lo ^ 16));
+    (i < kFR ? o.a[i < kFR ? i : 0] : o.b[i < kFR ? 0 : j]) =
         v8i{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
   };
 
@@ -491,26 +538,25 @@ __global__ __launch_bounds__(TT::kThreads, TT::kResident) void tile_kernel(Linea
   };
   auto x_scale = [&](const Operands &o, int j) { return o.sx >> (8 * j) & 255; };
 
-  // Step s: its products, and between them the copies of step s + kStages and
-  // the reads of step s + 1, the reads in the first half so that the barrier
-  // does not wait for them.  A burst of copies in front of the products keeps
-  // the wave's issue waiting behind the other waves' bursts.
+  // A step's products, and between them the copies and the reads that belong to
+  // it, the reads in the first half so that the barrier does not wait for them.
+  // A burst of copies in front of the products keeps the wave's issue waiting
+  // behind the other waves' bursts.
   constexpr int kProducts = kFR * kFC;
-  auto between = [&](int p, int s, Operands &next, bool more, bool last) {
+  auto between = [&](int p, auto &&read_one, auto &&copy_one) {
     constexpr int kHalf = kProducts > 1 ? kProducts / 2 : 1;
-    if (!last && p < kHalf)
+    if (p < kHalf)
 #pragma unroll
-      for (int k = p * kReads / kHalf; k < (p + 1) * kReads / kHalf; ++k) read(s + 1, k, next);
-    if (more)
+      for (int k = p * kReads / kHalf; k < (p + 1) * kReads / kHalf; ++k) read_one(k);
 #pragma unroll
-      for (int k = p * kCopies / kProducts; k < (p + 1) * kCopies / kProducts; ++k)
-        copy(s + kS, k);
+    for (int k = p * TT::kCopies / kProducts; k < (p + 1) * TT::kCopies / kProducts; ++k)
+      copy_one(k);
   };
-  auto step = [&](auto plain, int s, const Operands &o, Operands &next, bool more, bool last) {
+  auto step = [&](auto plain, const Operands &o, auto &&read_one, auto &&copy_one) {
     if constexpr (kOut == AF1_SRC_BF16) {
 #pragma unroll
       for (int p = 0; p < kProducts; ++p) {
-        between(p, s, next, more, last);
+        between(p, read_one, copy_one);
         product8(o, p / kFC, p % kFC);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -524,7 +570,7 @@ __global__ __launch_bounds__(TT::kThreads, TT::kResident) void tile_kernel(Linea
       for (int p = 0; p < kProducts; ++p) {
         const int i = p / kFC, j = p % kFC;
         if (j == 0) to_bf16<kWFormat>(o.a[i], kPlain ? scale_of(o.sw) : 1.f, a);
-        between(p, s, next, more, last);
+        between(p, read_one, copy_one);
         v16f t = kPlain ? acc[i][j] : v16f{};
 #pragma unroll
         for (int q = 0; q < 4; ++q)
@@ -539,35 +585,91 @@ __global__ __launch_bounds__(TT::kThreads, TT::kResident) void tile_kernel(Linea
     }
   };
 
-  // copies of the steps behind the next one
-  constexpr int kAhead = (kS - 2) * kCopies;
-  const int blocks = J1 - J0, steps = 2 * blocks;
-  for (int s = 0; s < min(kS, steps); ++s)
-#pragma unroll
-    for (int k = 0; k < kCopies; ++k) copy(s, k);
-  step_barrier<0>();
+  constexpr int kXC = TT::kXCopies + 2, kWC = TT::kWCopies;
+  // Copies in flight that a step does not wait for.  By blocks: the last step's
+  // and, since a step asks for W after the tokens, W's of the step before.  By
+  // halves: the last two steps'.
+  constexpr int kBehind = TT::kBlocks ? kXC + 2 * kWC : 2 * (kXC + kWC);
   Operands o0, o1;
+  auto start_x = [&](int s) {
 #pragma unroll
-  for (int k = 0; k < kReads; ++k) read(0, k, o0);
+    for (int k = 0; k < kXC; ++k) copy_x(s, s, k);
+  };
+  auto start_w = [&](int slot, int J, int q) {
+#pragma unroll
+    for (int k = 0; k < kWC; ++k) copy_w(slot, J, q, k);
+  };
+  // what the first step needs, then the rest of the ring
+  start_x(0);
+  start_w(0, 0, 0);
+  if constexpr (TT::kBlocks) {
+    start_w(0, 0, 1);
+    start_x(1);
+    start_x(2);
+    start_w(1, 1, 0);
+    start_w(1, 1, 1);
+    start_w(2, 2, 0);
+    step_barrier<2 * kXC + 3 * kWC>();
+  } else {
+#pragma unroll
+    for (int s = 1; s < 4; ++s) {
+      start_x(s);
+      start_w(s, s >> 1, s & 1);
+    }
+    step_barrier<3 * (kXC + kWC)>();
+  }
+#pragma unroll
+  for (int k = 0; k < kReads; ++k) read(0, 0, 0, k, o0);
+
   auto run = [&](auto plain) {
-    int J = 0;
-    for (; 2 * J + 1 + kS < steps; ++J) {
-      step_barrier<kAhead>();
-      step(plain, 2 * J, o0, o1, true, false);
-      step_barrier<kAhead>();
-      step(plain, 2 * J + 1, o1, o0, true, false);
+    int ws = 0, xs = 0;  // ring slots of W and of the tokens in step 2 J
+    const auto after = [](int slot) { return slot == TT::kSlots - 1 ? 0 : slot + 1; };
+#pragma unroll 1
+    for (int J = 0; J < blocks; ++J) {
+      const int x1 = after(xs), x2 = after(x1);
+      step_barrier<kBehind>();
+      if constexpr (TT::kBlocks) {
+        const int wn = after(ws), wp = after(wn);
+        step(
+            plain, o0, [&](int k) { read(ws, x1, 1, k, o1); },
+            [&](int k) {
+              if (k < kXC)
+                copy_x(xs, 2 * J + 3, k);
+              else
+                copy_w(wp, J + 2, 1, k - kXC);
+            });
+        step_barrier<kBehind>();
+        step(
+            plain, o1, [&](int k) { read(wn, x2, 0, k, o0); },
+            [&](int k) {
+              if (k < kXC)
+                copy_x(x1, 2 * J + 4, k);
+              else
+                copy_w(ws, J + 3, 0, k - kXC);
+            });
+        ws = wn;
+      } else {
+        step(
+            plain, o0, [&](int k) { read(x1, x1, 0, k, o1); },
+            [&](int k) {
+              if (k < kXC)
+                copy_x(xs, 2 * J + 4, k);
+              else
+                copy_w(xs, J + 2, 0, k - kXC);
+            });
+        step_barrier<kBehind>();
+        step(
+            plain, o1, [&](int k) { read(x2, x2, 0, k, o0); },
+            [&](int k) {
+              if (k < kXC)
+                copy_x(x1, 2 * J + 5, k);
+              else
+                copy_w(x1, J + 2, 1, k - kXC);
+            });
+      }
+      xs = x2;
     }
-    // nothing more to copy: what is left has been on its way for long
-    for (; J < blocks - 1; ++J) {
-      step_barrier<0>();
-      step(plain, 2 * J, o0, o1, false, false);
-      step_barrier<0>();
-      step(plain, 2 * J + 1, o1, o0, false, false);
-    }
-    step_barrier<0>();
-    step(plain, 2 * J, o0, o1, false, false);
-    step_barrier<0>();
-    step(plain, 2 * J + 1, o1, o0, false, true);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   };
   if constexpr (kOut == AF1_SRC_BF16) {
     run(std::true_type{});
@@ -1127,13 +1229,13 @@ hipError_t launch_linear(const af1_fp8_matrix &W, const void *x, int x_dtype, in
   switch (plan.form) {
     case kFew: return launch_few<kXFormat, kWFormat, kOut>(few, s);
     case kTiles64:
-      return launch_tiles<Tile<128, 64, 2, 2, 8>, kWFormat, kXFormat, kOut>(g, plan.splits, parts, s);
+      return launch_tiles<Tile<128, 64, 2, 2>, kWFormat, kXFormat, kOut>(g, plan.splits, parts, s);
     case kTiles128:
-      return launch_tiles<Tile<128, 128, 2, 2, 4>, kWFormat, kXFormat, kOut>(g, plan.splits, parts, s);
+      return launch_tiles<Tile<128, 128, 2, 2>, kWFormat, kXFormat, kOut>(g, plan.splits, parts, s);
     default: break;
   }
   if constexpr (kOut == AF1_SRC_BF16)
-    return launch_tiles<Tile<256, 256, 2, 2, 4>, kWFormat, kXFormat, kOut>(g, plan.splits, parts, s);
+    return launch_tiles<Tile<256, 256, 2, 2>, kWFormat, kXFormat, kOut>(g, plan.splits, parts, s);
   else
     return hipErrorInvalidValue;
 }

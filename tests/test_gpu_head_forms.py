@@ -51,6 +51,14 @@ def test_form(plan, ydtype, form, split, T, m, n):
     assert torch.equal(layer.forward(x.to("cuda"), dtype=ydtype), out)
 
 
+@pytest.mark.parametrize("n", [1, 130, 300, 400, 520])
+def test_fewer_column_blocks_than_the_ring(plan, n):
+    assert plan(8200, n, 500, af1.AF1_SRC_BF16) == (LARGE_TILES, False)
+    check_linear(500, 8200, n)
+    check_linear(45, 300, n)
+    check_linear(140, 777, n, ydtype=torch.float32)
+
+
 def test_mixed_formats_in_tiles(plan):
     assert plan(8200, 600, 500, af1.AF1_SRC_BF16)[0] == LARGE_TILES
     check_linear(500, 8200, 600, "e4m3", "e5m2", torch.float32, torch.bfloat16)
