@@ -161,9 +161,21 @@ class Fp8Linear:
         return cls(Fp8Matrix.quantize(w, fmt, stream=stream))
 
     def transposed(self, stream=None):
-        """The weight transposed, made once (the weight is frozen)."""
+        """The weight transposed, made once (the weight is frozen) and complete
+        when this returns, since calls on any stream use it from then on.  The
+        first call, or the first input_grad, cannot be captured into a graph:
+        the copy would exist only after a replay."""
         if self._T is None:
-            self._T = self.weight.transpose(stream)
+            dev = self.weight.device
+            if isinstance(stream, int):
+                stream = (torch.cuda.ExternalStream(stream, dev) if stream
+                          else torch.cuda.default_stream(dev))
+            with _on(dev, stream):
+                _need(not torch.cuda.is_current_stream_capturing(),
+                      "call transposed() before input_grad is captured into a graph")
+                T = self.weight.transpose()
+                torch.cuda.current_stream().synchronize()
+            self._T = T
         return self._T
 
     def workspace(self, T, grad=False):

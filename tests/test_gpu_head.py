@@ -544,6 +544,32 @@ def test_other_stream():
     assert torch.isfinite(d).all()
 
 
+def test_transposed_weight_is_not_captured():
+    """The transposed weight is made outside a graph, and once made it is used
+    by calls on other streams."""
+    layer = O.Fp8Linear.from_dense(randn(1, 300, 515).to("cuda"))
+    dy = randn(2, 45, 300).to("cuda")
+    dx = torch.zeros((45, 515), dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(ValueError, match="transposed"):
+            layer.input_grad(dy, dx)
+        dx.zero_()
+    side = torch.cuda.Stream()
+    first = layer.input_grad(dy, stream=side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(layer.input_grad(dy), first)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.input_grad(dy, dx)
+    for _ in range(3):
+        dx.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(dx, first)
+
+
 def test_captured_graphs():
     """A decode step and a training step captured, replayed on new inputs with
     eager work between the replays."""
