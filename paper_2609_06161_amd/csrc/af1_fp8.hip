@@ -209,34 +209,59 @@ inline size_t x_tile_bytes(int64_t n, int64_t T) {
   return (size_t)blocks_up(T) * blocks_up(n) * (kTileBytes + kBlk);
 }
 
-// Sixteen lanes a token and column block, eight columns a lane.
-template <typename D, int kFormat, bool kOperands>
-__global__ __launch_bounds__(256) void quantize_rows_kernel(const typename D::raw *x, int64_t T,
-                                                            int64_t n, XTiles out) {
-  const int64_t C = (n + kBlk - 1) / kBlk;
-  const int k = threadIdx.x & 15;
-  for (int64_t piece = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); piece < T * C;
-       piece += (int64_t)gridDim.x * 16) {
-    const int64_t t = piece / C, J = piece % C;
-    float v[8], amax = 0.f;
-    load8<D>(x + t * n + J * kBlk, k, n - J * kBlk, 0.f, v);
+// A token's piece of 128 columns, eight a lane of sixteen: codes and e.
+template <typename D, int kFormat>
+__device__ __forceinline__ uint2 round_piece(const Eight<D> &raw, int &e) {
+  float v[8], amax = 0.f;
+  widen<D>(raw, v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_abs(v[i]));
+  for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_abs(v[i]));
 #pragma unroll
-    for (int off = 8; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 16));
-    const int e = block_exponent<kFormat>(amax);
-    const uint2 codes = encode8<kFormat>(v, pow2(-e));
-    if constexpr (kOperands) {
-      *reinterpret_cast<uint2 *>(out.codes + operand_at((int)J, (int)t, k)) = codes;
-      if (k == 0) out.codes[C * 2048 + J * 16 + t] = (uint8_t)(e + 127);
-      continue;
-    }
+  for (int off = 8; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 16));
+  e = block_exponent<kFormat>(amax);
+  return encode8<kFormat>(v, pow2(-e));
+}
+
+// One workgroup a column block and 16 kPieces tokens; a lane's pieces are loaded
+// together.  Bound by memory, with four pieces: 34 us for 1000 x 50257 bf16 (43
+// with a 64-bit division a piece).  Few tokens are bound by latency and take one
+// piece a lane, for more waves: 500 x 8192 5.4 us, with four 6.0.
+template <typename D, int kFormat, int kPieces>
+__global__ __launch_bounds__(256) void quantize_tokens_kernel(const typename D::raw *x, int64_t T,
+                                                              int64_t n, XTiles out) {
+  const int C = (int)((n + kBlk - 1) / kBlk), J = blockIdx.x, k = threadIdx.x & 15;
+  const int64_t t0 = (int64_t)blockIdx.y * (16 * kPieces) + (threadIdx.x >> 4);
+  Eight<D> raw[kPieces];
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i)
+    raw[i] = load_raw_to<D>(x + min(t0 + 16 * i, T - 1) * n + J * kBlk, k, n - J * kBlk, 0.f);
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    int e;
+    const uint2 codes = round_piece<D, kFormat>(raw[i], e);
+    const int64_t t = t0 + 16 * i;
+    if (t >= T) break;
     const int64_t tile = t / kBlk * C + J;
     const int row = (int)(t % kBlk);
     *reinterpret_cast<uint2 *>(out.codes + tile * kTileBytes + (k >> 3) * kHalfBytes + row * 64 +
                                (k & 7) * 8) = codes;
     if (k == 0) out.scales[tile * kBlk + (row & 31) * 4 + (row >> 5)] = (uint8_t)(e + 127);
   }
+}
+
+// At most 16 tokens, as operands; sixteen pieces a workgroup.
+template <typename D, int kFormat>
+__global__ __launch_bounds__(256) void quantize_operands_kernel(const typename D::raw *x, int T,
+                                                                int64_t n, XTiles out) {
+  const int C = (int)((n + kBlk - 1) / kBlk), k = threadIdx.x & 15;
+  const int piece = blockIdx.x * 16 + (threadIdx.x >> 4);
+  if (piece >= T * C) return;
+  const int t = piece / C, J = piece % C;
+  int e;
+  const uint2 codes = round_piece<D, kFormat>(
+      load_raw_to<D>(x + t * n + J * kBlk, k, n - J * kBlk, 0.f), e);
+  *reinterpret_cast<uint2 *>(out.codes + operand_at(J, t, k)) = codes;
+  if (k == 0) out.codes[(int64_t)C * 2048 + J * 16 + t] = (uint8_t)(e + 127);
 }
 
 // The values of a lane's 32 codes at a power-of-two scale, for four matrix
@@ -1206,9 +1231,8 @@ hipError_t launch_linear(const af1_fp8_matrix &W, const void *x, int x_dtype, in
     return with_type(x_dtype, [&](auto d) {
       using D = decltype(d);
       if (!own) {
-        quantize_rows_kernel<D, kXFormat, true>
-            <<<(unsigned)((T * blocks_up(n) + 15) / 16), 256, 0, s>>>(
-                static_cast<const typename D::raw *>(x), T, n, few.xt);
+        quantize_operands_kernel<D, kXFormat><<<(unsigned)((T * blocks_up(n) + 15) / 16), 256, 0, s>>>(
+            static_cast<const typename D::raw *>(x), (int)T, n, few.xt);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
       }
@@ -1217,8 +1241,14 @@ hipError_t launch_linear(const af1_fp8_matrix &W, const void *x, int x_dtype, in
   }
   const hipError_t e = with_type(x_dtype, [&](auto d) {
     using D = decltype(d);
-    quantize_rows_kernel<D, kXFormat, false><<<grid_of((T * blocks_up(n) + 15) / 16), 256, 0, s>>>(
-        static_cast<const typename D::raw *>(x), T, n, xt);
+    const auto *rows = static_cast<const typename D::raw *>(x);
+    const unsigned C = (unsigned)blocks_up(n);
+    if (C * (T / 64) >= 8 * device_cus())
+      quantize_tokens_kernel<D, kXFormat, 4>
+          <<<dim3(C, (unsigned)((T + 63) / 64)), 256, 0, s>>>(rows, T, n, xt);
+    else
+      quantize_tokens_kernel<D, kXFormat, 1>
+          <<<dim3(C, (unsigned)((T + 15) / 16)), 256, 0, s>>>(rows, T, n, xt);
     return hipGetLastError();
   });
   if (e != hipSuccess) return e;
