@@ -311,8 +311,8 @@ AF1_API af1_status af1_pack_transpose(const uint32_t *src, int64_t rows, int64_t
  * after factorisation the paper freezes Bu and Bv and trains only s_out,
  * s_mid and s_in through the unchanged factorised graph.  These two calls
  * are that graph's forward and backward for T tokens of one layer; the
- * loss (a KL divergence to a full-precision teacher in the paper) and the
- * optimiser stay with the caller.
+ * loss (a KL divergence to a full-precision teacher in the paper;
+ * af1_distill_kl of af1_head.h) and the optimiser stay with the caller.
  *
  * af1_linear_forward_train -- y as af1_linear_gemm computes it (same
  * kernels and rounding, bit-identical y), and in `saved` the two pre-scale

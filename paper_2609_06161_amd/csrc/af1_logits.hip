@@ -15,6 +15,14 @@
 // Work is cut into parts of a row: whole rows when there are enough of them to
 // fill the device, parts of at least 2048 logits when there are few.  Parts'
 // results are joined in the parts' order.
+//
+// All of it is bound by memory where there are rows enough.  Log probabilities of
+// 1500 rows of 50257 bf16 with 5 alternatives: 40 us, 31 of them reading at the
+// rate of a copy; the rest is launch, first loads and the selection, which no
+// other row hides since all rows are resident at once.  One row of 128256 fp32
+// with 20: 7.3 us and 5.5 for the join (one workgroup and a search for every
+// alternative: 1672).  2048 rows of 32000 bf16: 28 us, the gradient 45 (262 MB,
+// some of it from the last-level cache).
 #include <math.h>
 
 #include "af1_head_device.h"
@@ -235,10 +243,10 @@ __device__ __forceinline__ void each_chunk(const typename D::raw *row, int64_t c
 // largest logit.  The k-th best of a wave's keys bounds the k-th best logit
 // from below, and so does the largest of the waves' bounds; only the threads at
 // or above it, at most k a wave, can hold one of the best: their chunks are
-// read again (from the caches), what reaches the bound is collected and sorted.  Keys are distinct, so equal logits need
-// no special case.  Rows with NaN, which the threads' largest logits do not
-// see, and rows with more to collect than there is room for are searched once
-// for every alternative.
+// read again (from the caches), what reaches the bound is collected and sorted.
+// Keys are distinct, so equal logits need no special case.  Rows with NaN, which
+// the threads' largest logits do not see, and rows with more to collect than
+// there is room for are searched once for every alternative.
 // ---------------------------------------------------------------------------
 
 constexpr int kMaxFound = 512;  // collected logits; beyond it, one at a time
@@ -537,7 +545,9 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(
 // statistics, waits for the others' and joins them all in the parts' order.
 // Waiting is bounded: statistics that do not arrive (their block has found no
 // place on the device yet) are computed by the block that misses them, from the
-// logits, with the same operations.
+// logits, with the same operations.  2048 rows of 128256 bf16 with the gradient:
+// 327 us, 4.8 TB/s (reading both rows again for the second pass: 517); 45 rows of
+// 50257 fp32 15 us.
 // ---------------------------------------------------------------------------
 
 struct KlArgs {
