@@ -105,7 +105,9 @@ AF1_API af1_status af1_fp8_transpose(const af1_fp8_matrix *W, uint8_t *codes, ui
  *       y's.  Use e5m2, with its wider range, for gradients.
  *   y : device, [T, m] of y_dtype (AF1_SRC_F32, AF1_SRC_BF16), written.
  *   T : 0 .. AF1_HEAD_MAX_TOKENS.
- *   ws: device, at least af1_fp8_linear_workspace_bytes(m, n, T) bytes.
+ *   ws: device, at least af1_fp8_linear_workspace_bytes(m, n, T) bytes.  Fewer
+ *       tokens may need more (they are split over more ranges of columns): one
+ *       workspace for calls of several T has the largest of their sizes.
  * Products are exact and accumulated in fp32 on the matrix cores.  The input
  * gradient dx = dy W is the same call with the transposed matrix.  y must not
  * overlap x, W or ws.

@@ -181,10 +181,9 @@ class Fp8Linear:
     def workspace(self, T, grad=False):
         """A workspace for calls of up to T tokens."""
         m, n = (self.n, self.m) if grad else (self.m, self.n)
-        need = head.af1_fp8_linear_workspace_bytes(m, n, T)
-        _need(need > 0 or 0 <= T <= head.AF1_HEAD_MAX_TOKENS, f"T must be at most "
-              f"{head.AF1_HEAD_MAX_TOKENS}")
-        return torch.empty(max(need, 16), dtype=torch.uint8, device=self.weight.device)
+        _need(0 <= T <= head.AF1_HEAD_MAX_TOKENS, f"T must be at most {head.AF1_HEAD_MAX_TOKENS}")
+        return torch.empty(max(workspace_up_to(m, n, T), 16), dtype=torch.uint8,
+                           device=self.weight.device)
 
     def forward(self, x, y=None, ws=None, fmt="e4m3", dtype=torch.bfloat16, stream=None):
         """[T, n] -> [T, m] of y's type, or of `dtype` (float32, bfloat16)."""
@@ -193,6 +192,18 @@ class Fp8Linear:
     def input_grad(self, dy, dx=None, ws=None, fmt="e5m2", dtype=torch.bfloat16, stream=None):
         """dx = dy W, [T, m] -> [T, n]."""
         return _linear(self.transposed(stream), dy, dx, ws, fmt, dtype, stream)
+
+
+def workspace_up_to(m, n, T):
+    """Bytes that cover every 8-bit linear of 1 to T tokens.  Fewer tokens may
+    need more: they are split over more ranges of columns.  Between these steps
+    the ranges only become fewer, so a step's need grows at most as its tokens."""
+    need = head.af1_fp8_linear_workspace_bytes(m, n, min(T, 16))
+    for first, last in [(17, 32), (33, 64)] + [(t, t + 63) for t in range(65, T + 1, 64)]:
+        if first <= T:
+            here = head.af1_fp8_linear_workspace_bytes(m, n, first)
+            need = max(need, -(-here * min(last, T) // first))
+    return need
 
 
 def _linear(W, x, y, ws, fmt, dtype, stream):

@@ -544,6 +544,41 @@ def test_other_stream():
     assert torch.isfinite(d).all()
 
 
+def test_one_workspace_for_fewer_tokens():
+    """A workspace for 500 tokens serves calls of fewer, which need more of it."""
+    layer = O.Fp8Linear.from_dense(randn(3, 4096, 4096).to("cuda"))
+    ws = layer.workspace(500)
+    for T in (500, 130, 45, 17, 1):
+        x = randn(T, T, 4096).to("cuda")
+        assert torch.equal(layer.forward(x, ws=ws), layer.forward(x))
+
+
+def test_two_calls_at_once():
+    """Calls that overlap in time on two streams give what they give alone; the
+    divergence's rows are work of several blocks that wait for each other."""
+    layer = O.Fp8Linear.from_dense(randn(4, 3001, 1000).to("cuda"))
+    x = [randn(5 + i, 45, 1000).to("cuda") for i in range(2)]
+    z = [randn(7 + i, 40, 130000).to("cuda") for i in range(3)]
+    y = torch.zeros(40, dtype=torch.int64, device="cuda")
+
+    def calls(i):
+        kl, grad = O.distill_kl(z[i], z[2])
+        p = O.token_logprobs(z[i], y, 7)
+        return [kl, grad, p.logprob, p.entropy, p.top_index, layer.forward(x[i])]
+
+    alone = [calls(0), calls(1)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(4):
+        got = [None, None]
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i] = calls(i)
+        torch.cuda.synchronize()
+        for g, w in zip(got[0] + got[1], alone[0] + alone[1]):
+            assert torch.equal(g, w)
+
+
 def test_transposed_weight_is_not_captured():
     """The transposed weight is made outside a graph, and once made it is used
     by calls on other streams."""

@@ -194,3 +194,12 @@ def test_tensor_checks():
                  lambda: output.Fp8Matrix(8, 8, "int8", z, z)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("m,n", [(4096, 4096), (8192, 8192), (1024, 50257), (50257, 4096),
+                                 (14336, 4096), (129, 2000), (20, 70)])
+def test_one_workspace_for_fewer_tokens(m, n):
+    need = [head.af1_fp8_linear_workspace_bytes(m, n, t) for t in range(1, 1101)]
+    for T in (1, 5, 16, 17, 32, 33, 40, 64, 65, 100, 128, 129, 200, 257, 500, 640, 1000, 1100):
+        assert output.workspace_up_to(m, n, T) >= max(need[:T])
+    assert output.workspace_up_to(m, n, 0) == 0
