@@ -897,10 +897,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewArgs g) {
 // workspace), more are rounded by a launch in front (kOwnPieces).  A ring
 // of kRing blocks is in flight a wave, across the ends of strips: memory sees
 // one unbroken stream.  128256 x 4096: 101 us for one token, 108 for twelve (525
-// MB, 5.2 and 4.9 TB/s); 1024 x 4096 5.4 us, which is latency.  When there are fewer strips than waves, kSplit waves
-// share a strip, every kSplit-th block each, and add their sums in LDS in
-// order; rows too long for LDS are taken that way too, a chunk of columns at a
-// time.
+// MB, 5.2 and 4.9 TB/s); 1024 x 4096 5.4 us, which is latency.  When there are
+// fewer strips than waves, kSplit waves share a strip, every kSplit-th block
+// each, and add their sums in LDS in order; rows too long for LDS are taken that
+// way too, a chunk of columns at a time.
 // ---------------------------------------------------------------------------
 
 constexpr int kStripWaves = 8;

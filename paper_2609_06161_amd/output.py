@@ -265,7 +265,7 @@ def _logprobs_call(logits, rows, targets, k, scale, ws, stream):
     # one block: the saved rows and the workspace first, which are aligned to 16
     # bytes, then what belongs to tokens
     saved, own, entropy, lse, logprob, top = torch.empty(
-        (7 + k) * T + need // 4, dtype=torch.float32, device=dev).split(
+        (7 + k) * T + need // 4, dtype=torch.float32, device=dev).split_with_sizes(
             (4 * T, need // 4, T, T, T, k * T))
     index = None
     if targets is None:
@@ -303,8 +303,10 @@ def token_logprobs_backward(logits, targets, result, g_logprob=None, g_entropy=N
 
 
 def _gradient(out, logits):
+    """(gradient, its row stride)."""
     if out is None:
         out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        return out, logits.shape[1]
     _need(out.dtype == logits.dtype and out.shape == logits.shape
           and out.device == logits.device, "the gradient must match the logits")
     return out, _logits(out, "the gradient")[3]
@@ -324,11 +326,14 @@ def distill_kl(student, teacher, scale=1.0, weight=None, grad=True, dstudent=Non
     _array(weight, "weight", dev, torch.float32, (T,))
 
     def call(stream):
-        kl, out, ldd = torch.empty(T, dtype=torch.float32, device=dev), None, 0
+        out, ldd = None, 0
         if grad or dstudent is not None:
             out, ldd = _gradient(dstudent, student)
-        wk, size = _workspace(ws, head.af1_distill_kl_workspace_bytes(T, V) if ws is None else 0,
-                              dev)
+        need = head.af1_distill_kl_workspace_bytes(T, V) if ws is None else 0
+        # one block, the workspace first for its alignment
+        wk, kl = torch.empty(need // 4 + T, dtype=torch.float32, device=dev).split_with_sizes(
+            (need // 4, T))
+        wk, size = (wk, need) if ws is None else _workspace(ws, 0, dev)
         head.af1_distill_kl(student, teacher, dtype, T, V, ld_s, ld_t, scale, weight, kl, out, ldd,
                             wk, size, stream)
         return kl, out
