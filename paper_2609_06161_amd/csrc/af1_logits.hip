@@ -20,7 +20,7 @@
 // 1500 rows of 50257 bf16 with 5 alternatives: 40 us, 31 of them reading at the
 // rate of a copy; the rest is launch, first loads and the selection, which no
 // other row hides since all rows are resident at once.  One row of 128256 fp32
-// with 20: 7.3 us and 5.5 for the join (one workgroup and a search for every
+// with 20: 11 us in two launches (one workgroup and a search for every
 // alternative: 1672).  2048 rows of 32000 bf16: 28 us, the gradient 45 (262 MB,
 // some of it from the last-level cache).
 #include <math.h>
@@ -155,6 +155,11 @@ __device__ __forceinline__ uint64_t order_key(float x, int64_t index) {
   return (uint64_t)u << 32 | (uint32_t)~(uint32_t)index;
 }
 __device__ __forceinline__ uint32_t key_index(uint64_t key) { return ~(uint32_t)key; }
+// The logit itself (0 for -0).
+__device__ __forceinline__ float key_logit(uint64_t key) {
+  const uint32_t u = (uint32_t)(key >> 32);
+  return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
 
 template <int kV>
 struct Int {
@@ -179,22 +184,36 @@ __device__ __forceinline__ float log_prob(float x, const Stat &s, float lnZ, flo
   return empty(s) ? -kInf : fmaf(x - s.m, scale, -lnZ);
 }
 
+// A row's target and its logit, read before the statistics are there.
+struct Target {
+  int64_t index = -1;
+  float logit = 0.f;
+};
 template <typename D>
-__device__ void write_row(const RowOut &o, const typename D::raw *row, int64_t r, int64_t V,
-                          const Stat &s) {
+__device__ __forceinline__ Target target_of(const RowOut &o, const typename D::raw *row, int64_t r,
+                                            int64_t V) {
+  Target t;
+  if (o.logprob && threadIdx.x == 0) {
+    t.index = o.targets[r];
+    if (t.index >= 0 && t.index < V) t.logit = D::get(row[t.index]);
+  }
+  return t;
+}
+
+__device__ void write_row(const RowOut &o, const Target &t, int64_t r, int64_t V, const Stat &s) {
   const float lnZ = logf(s.Z);
   const float H = empty(s) ? 0.f : lnZ - kLn2 * (s.W / s.Z);
   if (o.entropy) o.entropy[r] = H;
   if (o.lse) o.lse[r] = empty(s) ? -kInf : s.m * o.scale + lnZ;
   if (o.saved)
     reinterpret_cast<float4 *>(o.saved)[r] = make_float4(s.m, s.Z, H, log2f(s.Z));
-  if (o.logprob) {
-    const int64_t y = o.targets[r];
-    o.logprob[r] = y < 0    ? 0.f
-                   : y >= V ? __builtin_nanf("")
-                            : log_prob(D::get(row[y]), s, lnZ, o.scale);
-  }
+  if (o.logprob)
+    o.logprob[r] = t.index < 0    ? 0.f
+                   : t.index >= V ? __builtin_nanf("")
+                                  : log_prob(t.logit, s, lnZ, o.scale);
 }
+
+constexpr int kMaxParts = 64;  // of a row: one for each lane of the joining wave
 
 // A row's parts: `size` chunks of eight logits each (the last may be short).
 struct Parts {
@@ -369,8 +388,9 @@ __device__ uint64_t part_top(const typename D::raw *row, int64_t c0, int64_t c1,
   if (threadIdx.x == 0) l.bound = bound;
   if (mine != 0 && mine >= bound) l.holders[atomicAdd(&l.n_holders, 1)] = threadIdx.x;
   __syncthreads();
-  const int64_t each = (c1 - c0 + kThreads - 1) / kThreads;
-  for (int64_t i = threadIdx.x; i < l.n_holders * each; i += kThreads) {
+  // at most 128 threads and 2^13 chunks each
+  const unsigned each = (unsigned)(c1 - c0 + kThreads - 1) / kThreads;
+  for (unsigned i = threadIdx.x; i < l.n_holders * each; i += kThreads) {
     const int64_t c = c0 + l.holders[i / each] + i % each * kThreads;
     if (c >= c1) continue;
     float x[8];
@@ -392,14 +412,12 @@ __device__ uint64_t part_top(const typename D::raw *row, int64_t c0, int64_t c1,
   return threadIdx.x < 64 ? sort_found(l) : 0;
 }
 
-template <typename D>
-__device__ __forceinline__ void write_top(const RowOut &o, const typename D::raw *row, int64_t r,
-                                          const Stat &s, uint64_t key) {
+__device__ __forceinline__ void write_top(const RowOut &o, int64_t r, const Stat &s, uint64_t key) {
   if ((int)threadIdx.x >= o.k) return;
   const bool there = key != 0;
   o.top_index[r * o.k + threadIdx.x] = there ? (int64_t)key_index(key) : -1;
   o.top_logprob[r * o.k + threadIdx.x] =
-      there ? log_prob(D::get(row[key_index(key)]), s, logf(s.Z), o.scale) : -kInf;
+      there ? log_prob(key_logit(key), s, logf(s.Z), o.scale) : -kInf;
 }
 
 // What the parts of a row leave for the launch that joins them.
@@ -418,6 +436,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const typename D::ra
   const int part = blockIdx.x % parts.count;
   const typename D::raw *row = z + r * ld;
   const int64_t c0 = part * parts.size, c1 = min(c0 + parts.size, (V + 7) / 8);
+  const Target target = parts.count == 1 ? target_of<D>(o, row, r, V) : Target{};
   Stat s = no_logits();
   float best = -kInf;
   int chunk = -1;
@@ -437,8 +456,8 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const typename D::ra
   uint64_t key = 0;
   if constexpr (kTop) key = part_top<D>(row, c0, c1, V, o.k, best, chunk, s.Z != s.Z, top);
   if (parts.count == 1) {
-    if (threadIdx.x == 0) write_row<D>(o, row, r, V, s);
-    if constexpr (kTop) write_top<D>(o, row, r, s, key);
+    if (threadIdx.x == 0) write_row(o, target, r, V, s);
+    if constexpr (kTop) write_top(o, r, s, key);
   } else {
     if (threadIdx.x == 0) po.stats[blockIdx.x] = s;
     if (kTop && (int)threadIdx.x < o.k) po.keys[(int64_t)blockIdx.x * o.k + threadIdx.x] = key;
@@ -461,30 +480,44 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(const typename 
   __shared__ TopLds l;
   const int64_t r = blockIdx.x;
   const typename D::raw *row = z + r * ld;
-  const Stat s = join_parts<true>(po.stats + r * parts, parts, c);
-  if (threadIdx.x == 0) write_row<D>(o, row, r, V, s);
+  // everything is asked for at once
+  const uint64_t *keys = po.keys + r * parts * o.k;
+  constexpr int kEach = kTop ? kMaxParts * AF1_HEAD_MAX_TOP / kThreads : 1;
+  uint64_t mine[kEach], first = 0;
   if constexpr (kTop) {
-    const uint64_t *keys = po.keys + r * parts * o.k;
+    if ((int)threadIdx.x < parts) first = keys[threadIdx.x * o.k];
+#pragma unroll
+    for (int a = 0; a < kEach; ++a) {
+      const int i = threadIdx.x + a * kThreads;
+      mine[a] = i < parts * o.k ? keys[i] : 0;
+    }
+  }
+  const Target target = target_of<D>(o, row, r, V);
+  const Stat s = join_parts<true>(po.stats + r * parts, parts, c);
+  if (threadIdx.x == 0) write_row(o, target, r, V, s);
+  if constexpr (kTop) {
     if (threadIdx.x < 64) {
-      const uint64_t v = sort64((int)threadIdx.x < parts ? keys[threadIdx.x * o.k] : 0);
+      const uint64_t v = sort64(first);
       // the list of a part with fewer than k logits ends in zeros
       if ((int)threadIdx.x == o.k - 1) l.bound = v;
       if (threadIdx.x == 0) l.n_found = 0;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < parts * o.k; i += kThreads) collect(l, keys[i]);
+#pragma unroll
+    for (int a = 0; a < kEach; ++a) collect(l, mine[a]);
     __syncthreads();
     uint64_t key;
     if (l.n_found > kMaxFound)
       key = one_by_one(o.k, l, [&](uint64_t after) {
         uint64_t b = 0;
-        for (int i = threadIdx.x; i < parts * o.k; i += kThreads)
-          if (keys[i] < after) b = max64(b, keys[i]);
+#pragma unroll
+        for (int a = 0; a < kEach; ++a)
+          if (mine[a] < after) b = max64(b, mine[a]);
         return b;
       });
     else
       key = threadIdx.x < 64 ? sort_found(l) : 0;
-    write_top<D>(o, row, r, s, key);
+    write_top(o, r, s, key);
   }
 }
 
@@ -841,7 +874,6 @@ Parts plan_parts(int64_t T, int64_t V, int64_t want, int most) {
   const int64_t size = ((chunks + n - 1) / n + kThreads - 1) / kThreads * kThreads;
   return Parts{(int)((chunks + size - 1) / size), size};
 }
-constexpr int kMaxParts = 64;  // one for each lane of the joining wave
 
 size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 
