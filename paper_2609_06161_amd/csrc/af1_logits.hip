@@ -17,9 +17,9 @@
 // results are joined in the parts' order.
 //
 // All of it is bound by memory where there are rows enough.  Log probabilities of
-// 1500 rows of 50257 bf16 with 5 alternatives: 40 us, 31 of them reading at the
-// rate of a copy; the rest is launch, first loads and the selection, which no
-// other row hides since all rows are resident at once.  One row of 128256 fp32
+// 1500 rows of 50257 bf16: 29.6 us, the rate of a copy; with 5 alternatives 35.5,
+// with 20 39.6: the selection comes at the end of rows that are all resident at
+// once, so none hides another's.  One row of 128256 fp32
 // with 20: 11 us in two launches (one workgroup and a search for every
 // alternative: 1672).  2048 rows of 32000 bf16: 28 us, the gradient 45 (262 MB,
 // some of it from the last-level cache).
@@ -261,8 +261,11 @@ __device__ __forceinline__ void each_chunk(const typename D::raw *row, int64_t c
 // Alternatives.  Every thread remembers the first of its chunks that holds its
 // largest logit.  The k-th best of a wave's keys bounds the k-th best logit
 // from below, and so does the largest of the waves' bounds; only the threads at
-// or above it, at most k a wave, can hold one of the best: their chunks are
-// read again (from the caches), what reaches the bound is collected and sorted.
+// or above it, at most k a wave, can hold one of the best: that chunk, or all of
+// a thread's if its second best reaches the bound too, is read again (from the
+// caches; a thread's chunks lie in different lines, and reading all of every
+// thread's took 52 us instead of 39.6 for 1500 rows of 50257 bf16 with 20), and
+// what reaches the bound is collected and sorted.
 // Keys are distinct, so equal logits need no special case.  Rows with NaN, which
 // the threads' largest logits do not see, and rows with more to collect than
 // there is room for are searched once for every alternative.
@@ -274,8 +277,8 @@ struct TopLds {
   uint64_t waves[kWaves], scratch[64];
   uint64_t found[kMaxFound];
   uint64_t bound;
-  int holders[kWaves * AF1_HEAD_MAX_TOP];
-  int n_holders, n_found;
+  int holders[kWaves * AF1_HEAD_MAX_TOP], chunks[kWaves * AF1_HEAD_MAX_TOP];
+  int n_holders, n_chunks, n_found;
 };
 
 __device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int mask) {
@@ -373,25 +376,33 @@ __device__ __forceinline__ uint64_t one_by_one(int k, TopLds &l, F &&next) {
 
 // In wave 0, lane i gets the i-th largest key of the chunks c0 .. c1 - 1 (i <
 // k).  best, chunk: this thread's largest logit and the first chunk with it
-// (chunk < 0: the thread has none).  odd: there may be NaN.
+// (chunk < 0: the thread has none); second: the largest of its other chunks.
+// odd: there may be NaN.
 template <typename D>
 __device__ uint64_t part_top(const typename D::raw *row, int64_t c0, int64_t c1, int64_t V, int k,
-                             float best, int64_t chunk, bool odd, TopLds &l) {
-  const uint64_t mine = chunk < 0 ? 0 : order_key(best, 8 * chunk + 7);
+                             float best, float second, int chunk, bool odd, TopLds &l) {
+  const uint64_t mine = chunk < 0 ? 0 : order_key(best, 8 * (int64_t)chunk + 7);
   const uint64_t v = sort64(mine);
   if ((int)(threadIdx.x & 63) == k - 1) l.waves[threadIdx.x >> 6] = v;
-  if (threadIdx.x == 0) l.n_holders = l.n_found = 0;
+  if (threadIdx.x == 0) l.n_holders = l.n_chunks = l.n_found = 0;
   __syncthreads();
   uint64_t bound = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) bound = max64(bound, l.waves[w]);
   if (threadIdx.x == 0) l.bound = bound;
-  if (mine != 0 && mine >= bound) l.holders[atomicAdd(&l.n_holders, 1)] = threadIdx.x;
+  if (mine != 0 && mine >= bound) {
+    // no bound has the logit NaN, and all chunks count
+    if (second < key_logit(bound))
+      l.chunks[atomicAdd(&l.n_chunks, 1)] = chunk;
+    else
+      l.holders[atomicAdd(&l.n_holders, 1)] = threadIdx.x;
+  }
   __syncthreads();
-  // at most 128 threads and 2^13 chunks each
-  const unsigned each = (unsigned)(c1 - c0 + kThreads - 1) / kThreads;
-  for (unsigned i = threadIdx.x; i < l.n_holders * each; i += kThreads) {
-    const int64_t c = c0 + l.holders[i / each] + i % each * kThreads;
+  // at most 128 of both, and 2^13 chunks each
+  const unsigned each = (unsigned)(c1 - c0 + kThreads - 1) / kThreads, ones = l.n_chunks;
+  for (unsigned i = threadIdx.x; i < ones + l.n_holders * each; i += kThreads) {
+    const unsigned j = i - ones;
+    const int64_t c = i < ones ? l.chunks[i] : c0 + l.holders[j / each] + j % each * kThreads;
     if (c >= c1) continue;
     float x[8];
     load8<D>(row, c, V, -kInf, x);
@@ -438,7 +449,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const typename D::ra
   const int64_t c0 = part * parts.size, c1 = min(c0 + parts.size, (V + 7) / 8);
   const Target target = parts.count == 1 ? target_of<D>(o, row, r, V) : Target{};
   Stat s = no_logits();
-  float best = -kInf;
+  float best = -kInf, second = -kInf;
   int chunk = -1;
   each_chunk<D>(row, c0, c1, V, [&](int i, const auto &x) {
     constexpr int kN = sizeof(x) / 32;
@@ -447,14 +458,17 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const typename D::ra
     for (int n = 0; n < kN; ++n) {
       const float m = max8(x[n]);
       if constexpr (kTop)
+      {
+        second = __builtin_amdgcn_fmed3f(m, best, second);
         if (chunk < 0 || m > best) best = m, chunk = i + n * kThreads;
+      }
       top = fmaxf(top, m);
     }
     add<true>(s, x, top, c);
   });
   s = block_join<true>(s, c, sh);
   uint64_t key = 0;
-  if constexpr (kTop) key = part_top<D>(row, c0, c1, V, o.k, best, chunk, s.Z != s.Z, top);
+  if constexpr (kTop) key = part_top<D>(row, c0, c1, V, o.k, best, second, chunk, s.Z != s.Z, top);
   if (parts.count == 1) {
     if (threadIdx.x == 0) write_row(o, target, r, V, s);
     if constexpr (kTop) write_top(o, r, s, key);
