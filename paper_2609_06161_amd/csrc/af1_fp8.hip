@@ -74,8 +74,8 @@ __device__ __forceinline__ float decode(uint32_t w) {
 // ---------------------------------------------------------------------------
 // Quantisation, reading back, transposition: one workgroup a tile, which it holds
 // in registers between the largest entry and the codes.  Bound by memory: 8192 x
-// 8192 bf16 in 44 us (201 MB, 4.6 TB/s), back in 30 (the codes from the last-level
-// cache).
+// 8192 bf16 there and back in 69 us (335 MB, the codes' second pass from the
+// last-level cache; 74 with the values not stored past the caches).
 // ---------------------------------------------------------------------------
 
 // Codes of eight values at 2^-e.
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t *codes,
           decode<kFormat, 2>(w[q].x) * scale, decode<kFormat, 3>(w[q].x) * scale,
           decode<kFormat, 0>(w[q].y) * scale, decode<kFormat, 1>(w[q].y) * scale,
           decode<kFormat, 2>(w[q].y) * scale, decode<kFormat, 3>(w[q].y) * scale};
-      store8<D>(at + 16 * q * cols, k, left, v);
+      store8<D, true>(at + 16 * q * cols, k, left, v);
     }
   }
 }

@@ -84,7 +84,8 @@ __device__ __forceinline__ void load8(const typename D::raw *row, int64_t c, int
   widen<D>(load_raw_to<D>(row, c, V, fill), x);
 }
 
-template <typename D>
+// kPast: past the caches.
+template <typename D, bool kPast = false>
 __device__ __forceinline__ void store8(typename D::raw *row, int64_t c, int64_t V,
                                        const float (&x)[8]) {
   if (8 * c + 8 <= V) {
@@ -96,7 +97,16 @@ __device__ __forceinline__ void store8(typename D::raw *row, int64_t c, int64_t 
       else
         e.w[i] = (uint32_t)D::put(x[2 * i]) | (uint32_t)D::put(x[2 * i + 1]) << 16;
     }
-    *reinterpret_cast<Eight<D> *>(row + 8 * c) = e;
+    if constexpr (kPast) {
+      // an element's alignment at most
+      typedef uint32_t raw4 __attribute__((ext_vector_type(4), aligned(2)));
+#pragma unroll
+      for (int i = 0; i < (int)(sizeof(e) / 16); ++i)
+        __builtin_nontemporal_store(raw4{e.w[4 * i], e.w[4 * i + 1], e.w[4 * i + 2], e.w[4 * i + 3]},
+                                    reinterpret_cast<raw4 *>(row + 8 * c) + i);
+    } else {
+      *reinterpret_cast<Eight<D> *>(row + 8 * c) = e;
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)

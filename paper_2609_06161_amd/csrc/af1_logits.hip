@@ -19,10 +19,14 @@
 // All of it is bound by memory where there are rows enough.  Log probabilities of
 // 1500 rows of 50257 bf16: 29.6 us, the rate of a copy; with 5 alternatives 35.5,
 // with 20 39.6: the selection comes at the end of rows that are all resident at
-// once, so none hides another's.  One row of 128256 fp32
-// with 20: 11 us in two launches (one workgroup and a search for every
-// alternative: 1672).  2048 rows of 32000 bf16: 28 us, the gradient 45 (262 MB,
-// some of it from the last-level cache).
+// once, so none hides another's.  One row of 128256 fp32 with 20: 11 us in two
+// launches (one workgroup and a search for every
+// alternative: 1672).  2048 rows of 32000 bf16: 26 us.
+//
+// Gradients are stored past the caches, which then still hold the logits of the
+// forward: forward and backward of 2048 rows of 32000 bf16 76 us, stored plainly
+// 89; 2048 rows of 128256 bf16 of the KL 321 and 328.  The product that reads the
+// gradient next is not slower for it (45 to 2048 rows, 32000 to 128256 wide).
 #include <math.h>
 
 #include "af1_head_device.h"
@@ -571,7 +575,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(
         for (int j = 0; j < 8; ++j)
           if (8 * i + j == y) d[j] += gl;
       }
-      store8<D>(out, i, V, d);
+      store8<D, true>(out, i, V, d);
     }
   });
 }
@@ -593,7 +597,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(
 // Waiting is bounded: statistics that do not arrive (their block has found no
 // place on the device yet) are computed by the block that misses them, from the
 // logits, with the same operations.  2048 rows of 128256 bf16 with the gradient:
-// 327 us, 4.8 TB/s (reading both rows again for the second pass: 517); 45 rows of
+// 321 us, 4.9 TB/s (reading both rows again for the second pass: 517); 45 rows of
 // 50257 fp32 15 us.
 // ---------------------------------------------------------------------------
 
@@ -830,7 +834,7 @@ __global__ __launch_bounds__(kThreads, 4) void kl_kernel(const typename D::raw *
       }
     }
     const int64_t i = c0 + threadIdx.x + j * kThreads;
-    if (ds && i < c1) store8<D>(ds + r * g.ldd, i, V, d);
+    if (ds && i < c1) store8<D, true>(ds + r * g.ldd, i, V, d);
   }
   A = wave_add(A);
   B = wave_add(B);
