@@ -66,7 +66,7 @@ def _run(call, device, stream, *args):
     smallest kernels, so it is left out where both are current already."""
     if stream is None:
         index = device.index
-        if index == torch.cuda.current_device():
+        if index == torch._C._cuda_getDevice():
             return call(*args, torch._C._cuda_getCurrentRawStream(index))
     with _on(device, stream):
         return call(*args, stream)
@@ -208,7 +208,8 @@ def workspace_up_to(m, n, T):
 
 def _linear(W, x, y, ws, fmt, dtype, stream):
     x_dtype, dev = _dense(x, "x"), W.codes.device
-    _need(fmt in FORMATS, f"fmt must be one of {tuple(FORMATS)}, not {fmt!r}")
+    if fmt not in FORMATS:
+        raise ValueError(f"fmt must be one of {tuple(FORMATS)}, not {fmt!r}")
     if x.dim() != 2 or x.shape[1] != W.cols or not x.is_contiguous() or x.device != dev:
         raise ValueError(f"x must be contiguous of shape [T, {W.cols}] on {dev}")
     if y is not None:
@@ -228,12 +229,17 @@ def _linear_call(W, x, x_dtype, fmt, y, dtype, ws, stream):
 
 def _logits(t, name):
     """(dtype code, T, V, row stride) of a [T, V] tensor whose rows may be apart."""
-    dtype = _dense(t, name)
-    _need(t.dim() == 2 and t.shape[1] >= 1, f"{name} must be [T, V]")
-    T, V = t.shape
-    _need(V == 1 or t.stride(1) == 1, f"{name}'s rows must be contiguous")
-    ld = t.stride(0) if T > 1 else V
-    _need(ld >= V, f"{name}'s rows must not overlap")
+    dtype, shape = _dense(t, name), t.shape
+    if len(shape) != 2 or shape[1] < 1:
+        raise ValueError(f"{name} must be [T, V]")
+    T, V = shape
+    ld, step = t.stride()
+    if V > 1 and step != 1:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    if T <= 1:
+        ld = V
+    elif ld < V:
+        raise ValueError(f"{name}'s rows must not overlap")
     return dtype, T, V, ld
 
 
@@ -254,7 +260,8 @@ def token_logprobs(logits, targets=None, k=0, scale=1.0, ws=None, stream=None):
     rows, dev = _logits(logits, "logits"), logits.device
     T = rows[1]
     _array(targets, "targets", dev, torch.int64, (T,))
-    _need(0 <= k <= head.AF1_HEAD_MAX_TOP, f"k must be in 0..{head.AF1_HEAD_MAX_TOP}, not {k}")
+    if not 0 <= k <= head.AF1_HEAD_MAX_TOP:
+        raise ValueError(f"k must be in 0..{head.AF1_HEAD_MAX_TOP}, not {k}")
     return _run(_logprobs_call, dev, stream, logits, rows, targets, k, scale, ws)
 
 
