@@ -1064,7 +1064,10 @@ auto with_format(int f, F &&g) {
 }
 
 constexpr int64_t kStripTokens = 16, kFewTokens = 32;
-constexpr int64_t kOwnPieces = 128;  // of x that a strip workgroup rounds itself
+// Pieces of x that every strip workgroup rounds itself: 4 tokens of 8192 x 8192
+// (256 pieces) take 20.0 us with a launch in front and 21.0 without, 8 of 4096 x
+// 4096 7.3 and 9.5.
+constexpr int64_t kOwnPieces = 128;
 
 // y = the partial sums' sum, in the ranges' order.
 template <typename D>
@@ -1169,10 +1172,16 @@ hipError_t launch_strips(const FewArgs &g, hipStream_t s) {
   return hipGetLastError();
 }
 
+// How many waves share a strip.  Each on its own where that leaves more than half
+// of the compute units a workgroup, since a second round of workgroups starts by
+// rounding x again (one token of 28672 x 8192: 37 us, shared by two 64; 24576 x
+// 4096 19 and 23); fewer strips are shared by as many waves as fill the device
+// (16384 x 4096: by two 13.9, alone 18.5; 8192 x 28672: by four 42, by eight 48;
+// 4096 x 4096: by eight 5.2, by four 6.9).
 template <typename D, int kXFormat, int kWFormat, int kOut>
 hipError_t launch_strip_form(const FewArgs &g, hipStream_t s) {
   const int64_t strips = (g.m + 15) / 16, cus = device_cus();
-  if (strips >= 8 * cus && blocks_up(g.n) <= kStripBlocks)
+  if (strips > 4 * cus && blocks_up(g.n) <= kStripBlocks)
     return launch_strips<D, kXFormat, kWFormat, kOut, 1>(g, s);
   if (strips >= 4 * cus) return launch_strips<D, kXFormat, kWFormat, kOut, 2>(g, s);
   if (strips >= 2 * cus) return launch_strips<D, kXFormat, kWFormat, kOut, 4>(g, s);
