@@ -146,7 +146,9 @@ class Fp8Matrix:
 class Fp8Linear:
     """y = x W^T with W an Fp8Matrix of m = rows by n = cols.  Activations are
     rounded to 8 bits inside the call, each token's 128 columns at a scale of
-    their own; sums are fp32."""
+    their own.  Sums are fp32 for outputs in fp32 and for up to 16 tokens; for
+    more tokens with outputs in bfloat16 (the default) each eight columns'
+    products are cut below 2^-13 of their largest before that (af1_fp8_linear)."""
 
     def __init__(self, weight, transposed=None):
         self.weight = weight
