@@ -20,15 +20,17 @@ def to_device(a: np.ndarray, device="cuda") -> torch.Tensor:
     return torch.from_numpy(a.view(_VIEW[a.dtype])).to(device)
 
 
-def on_stream(stream):
+def on_stream(stream, device=None):
     """Context in which the helpers below allocate their outputs and
     workspaces: the stream the kernels are launched on (torch's current one
-    when stream is None), so a zero-fill is ordered before the kernels and
-    the caching allocator does not hand the memory to other work while they
-    may still use it."""
-    if stream is None or isinstance(stream, int):
-        # an integer stream handle: the caller owns ordering and lifetimes
+    when stream is None; an integer is a stream's handle on `device`), so a
+    zero-fill is ordered before the kernels and the caching allocator does not
+    hand the memory to other work while they may still use it."""
+    if stream is None:
         return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = (torch.cuda.ExternalStream(stream, device) if stream
+                  else torch.cuda.default_stream(device))
     return torch.cuda.stream(stream)
 
 
@@ -58,7 +60,7 @@ class DeviceLayer:
 
     def gemv(self, x: torch.Tensor, y: torch.Tensor = None, ws: torch.Tensor = None, stream=None):
         b = x.shape[0]
-        with on_stream(stream):
+        with on_stream(stream, x.device):
             if y is None:
                 y = torch.empty((b, self.m), dtype=torch.int16, device=x.device)
             need = af1.af1_gemv_workspace_bytes(self.m, self.n, self.r, b)
@@ -70,7 +72,7 @@ class DeviceLayer:
 
     def gemm(self, x: torch.Tensor, y: torch.Tensor = None, ws: torch.Tensor = None, stream=None):
         T = x.shape[0]
-        with on_stream(stream):
+        with on_stream(stream, x.device):
             if y is None:
                 y = torch.empty((T, self.m), dtype=torch.int16, device=x.device)
             need = af1.af1_gemm_workspace_bytes(self.m, self.n, self.r, T)
@@ -93,7 +95,7 @@ class DeviceLayer:
 
     def forward_train(self, x, y=None, saved=None, ws=None, stream=None):
         T = x.shape[0]
-        with on_stream(stream):
+        with on_stream(stream, x.device):
             if y is None:
                 y = torch.empty((T, self.m), dtype=torch.int16, device=x.device)
             if saved is None:
@@ -111,7 +113,7 @@ class DeviceLayer:
         """dx ([T, n] bf16 patterns, or None) and the fp32 scale gradients
         (ds_out, ds_mid, ds_in)."""
         T = x.shape[0]
-        with on_stream(stream):
+        with on_stream(stream, x.device):
             BuT, BvT = self.transposed(stream)
             if dx is None and want_dx:
                 dx = torch.empty((T, self.n), dtype=torch.int16, device=x.device)
@@ -130,7 +132,7 @@ class DeviceLayer:
 def gemv_multi(layers, x: torch.Tensor, ys=None, ws: torch.Tensor = None, stream=None):
     """One decode step of several layers that read the same x (same n)."""
     b = x.shape[0]
-    with on_stream(stream):
+    with on_stream(stream, x.device):
         if ys is None:
             ys = [torch.empty((b, L.m), dtype=torch.int16, device=x.device) for L in layers]
         descs = [L.desc for L in layers]

@@ -56,7 +56,7 @@ def _workspace(ws, need, device):
 @contextlib.contextmanager
 def _on(device, stream):
     """The device of the tensors and the stream that the kernels run on."""
-    with torch.cuda.device(device), on_stream(stream):
+    with torch.cuda.device(device), on_stream(stream, device):
         yield
 
 
@@ -64,10 +64,12 @@ def _run(call, device, stream, *args):
     """call(*args, stream) on the tensors' device and the given stream, or that
     device's current one.  Entering a device and a stream costs as much as the
     smallest kernels, so it is left out where both are current already."""
-    if stream is None:
+    if stream is None or isinstance(stream, int):
         index = device.index
         if index == torch._C._cuda_getDevice():
-            return call(*args, torch._C._cuda_getCurrentRawStream(index))
+            current = torch._C._cuda_getCurrentRawStream(index)
+            if stream is None or stream == current:
+                return call(*args, current)
     with _on(device, stream):
         return call(*args, stream)
 
@@ -169,9 +171,6 @@ class Fp8Linear:
         the copy would exist only after a replay."""
         if self._T is None:
             dev = self.weight.device
-            if isinstance(stream, int):
-                stream = (torch.cuda.ExternalStream(stream, dev) if stream
-                          else torch.cuda.default_stream(dev))
             with _on(dev, stream):
                 _need(not torch.cuda.is_current_stream_capturing(),
                       "call transposed() before input_grad is captured into a graph")

@@ -1,0 +1,45 @@
+"""Which stream the tensor calls allocate on (CPU, torch's stream objects
+replaced): memory of a call that runs on a given stream has to come from that
+stream's pool, or it is handed to other work while the call still uses it."""
+import contextlib
+
+import pytest
+import torch
+
+from paper_2609_06161_amd import layer
+
+
+class Device:
+    index = 0
+
+
+@pytest.fixture
+def entered(monkeypatch):
+    """The streams that are entered, in order."""
+    seen = []
+
+    @contextlib.contextmanager
+    def stream(s):
+        seen.append(s)
+        yield
+        seen.append("left")
+
+    monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda h, device=None: ("external", h, device))
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: ("default", device))
+    return seen
+
+
+@pytest.mark.parametrize("handle,want", [(1234, ("external", 1234, Device)),
+                                         (0, ("default", Device))])
+def test_an_integer_is_a_streams_handle(entered, handle, want):
+    with layer.on_stream(handle, Device):
+        assert entered == [want]
+    assert entered == [want, "left"]
+
+
+def test_other_streams(entered):
+    with layer.on_stream(None, Device):
+        assert entered == []
+    with layer.on_stream("a stream"):
+        assert entered == ["a stream"]
