@@ -84,12 +84,19 @@ class DeviceLayer:
     # -- scale-only reconstruction: signs frozen, scales trained -----------
 
     def transposed(self, stream=None):
-        """(Bu^T, Bv^T) in the packed format, made once on the device."""
+        """(Bu^T, Bv^T) in the packed format, made once on the device and complete
+        when this returns, since calls on any stream use them from then on.  While
+        a graph is captured they are made in the graph and not kept: they would
+        hold nothing before a replay."""
         if getattr(self, "_T", None) is None:
-            BuT = torch.empty((self.r, self.m // 32), dtype=torch.int32, device=self.Bu.device)
-            BvT = torch.empty((self.n, self.r // 32), dtype=torch.int32, device=self.Bu.device)
-            af1.af1_pack_transpose(self.Bu, self.m, self.r, BuT, stream)
-            af1.af1_pack_transpose(self.Bv, self.r, self.n, BvT, stream)
+            with on_stream(stream, self.Bu.device):
+                BuT = torch.empty((self.r, self.m // 32), dtype=torch.int32, device=self.Bu.device)
+                BvT = torch.empty((self.n, self.r // 32), dtype=torch.int32, device=self.Bu.device)
+                af1.af1_pack_transpose(self.Bu, self.m, self.r, BuT, stream)
+                af1.af1_pack_transpose(self.Bv, self.r, self.n, BvT, stream)
+                if torch.cuda.is_current_stream_capturing():
+                    return BuT, BvT
+                torch.cuda.current_stream().synchronize()
             self._T = (BuT, BvT)
         return self._T
 

@@ -66,3 +66,35 @@ def test_reconstruction_on_an_integer_stream():
     want = step(None)
     for a, b in zip(late(step, torch.cuda.Stream()), want):
         assert torch.equal(a, b)
+
+
+def test_signs_are_transposed_for_every_stream():
+    """The first backward of a layer is captured, a later one runs on a stream
+    while another is busy: each has complete transposed signs."""
+    lin = synth.make_linear(9, 512, 768, 224, 45)
+    x = to_device(lin.x)
+    dy = randn(10, 45, 512).to(torch.bfloat16).to(DEV).view(torch.int16)
+    known = DeviceLayer.from_host(lin)
+    saved = known.forward_train(x)[1]
+    dx, grads = known.backward(x, dy, saved)
+    want = [dx, *grads]
+    layer = DeviceLayer.from_host(lin)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dx, grads = layer.backward(x, dy, saved)
+    held = [dx, *grads]
+    side = torch.cuda.Stream()
+    dx, grads = late(lambda s: layer.backward(x, dy, saved, stream=s), side)
+    for a, b in zip([dx, *grads], want):
+        assert torch.equal(a, b)
+    dx, grads = layer.backward(x, dy, saved)
+    for a, b in zip([dx, *grads], want):
+        assert torch.equal(a, b)
+    for _ in range(3):
+        for t in held:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, want):
+            assert torch.equal(a, b)

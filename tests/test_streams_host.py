@@ -6,7 +6,7 @@ import contextlib
 import pytest
 import torch
 
-from paper_2609_06161_amd import layer
+from paper_2609_06161_amd import layer, synth
 
 
 class Device:
@@ -43,3 +43,24 @@ def test_other_streams(entered):
         assert entered == []
     with layer.on_stream("a stream"):
         assert entered == ["a stream"]
+
+
+@pytest.mark.parametrize("capturing", [False, True])
+def test_transposed_signs_are_complete_before_they_are_kept(monkeypatch, capturing):
+    done = []
+
+    class Stream:
+        def synchronize(self):
+            done.append("complete")
+
+    monkeypatch.setattr(layer.af1, "af1_pack_transpose", lambda *a: done.append("moved"))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream())
+    lin = synth.make_linear(1, 64, 96, 32, 1)
+    L = layer.DeviceLayer.from_host(lin, device="cpu")
+    first, second = L.transposed(), L.transposed()
+    assert [t.shape for t in first] == [(32, 2), (96, 1)]
+    if capturing:       # made in each graph that needs them, kept by none
+        assert done == ["moved"] * 4 and first[0] is not second[0]
+    else:
+        assert done == ["moved"] * 2 + ["complete"] and first is second
