@@ -362,11 +362,12 @@ def reconstruction_step(layer, output, x, teacher, weight=None, scale=1.0, grads
     _need(output.n == layer.m, f"the head reads {output.n} features, the layer gives {layer.m}")
     _need(teacher.dtype in (torch.float32, torch.bfloat16), "teacher must be float32 or bfloat16")
     xb = x.view(torch.int16) if x.dtype == torch.bfloat16 else x
-    hidden, saved = layer.forward_train(xb, stream=stream)
-    logits = output.forward(hidden, dtype=teacher.dtype, stream=stream)
-    # the gradient takes the logits' place
-    kl, dlogits = distill_kl(logits, teacher, scale, weight, dstudent=logits, stream=stream)
-    dh = output.input_grad(dlogits, stream=stream)
-    dx, grads = layer.backward(xb, dh.view(torch.int16), saved, grads=grads,
-                               accumulate=accumulate, stream=stream, want_dx=want_dx)
+    with _on(x.device, stream):     # the layer's own calls stay on the current device
+        hidden, saved = layer.forward_train(xb)
+        logits = output.forward(hidden, dtype=teacher.dtype)
+        # the gradient takes the logits' place
+        kl, dlogits = distill_kl(logits, teacher, scale, weight, dstudent=logits)
+        dh = output.input_grad(dlogits)
+        dx, grads = layer.backward(xb, dh.view(torch.int16), saved, grads=grads,
+                                   accumulate=accumulate, want_dx=want_dx)
     return kl, dx, grads

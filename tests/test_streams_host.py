@@ -6,7 +6,7 @@ import contextlib
 import pytest
 import torch
 
-from paper_2609_06161_amd import layer, synth
+from paper_2609_06161_amd import layer, output, synth
 
 
 class Device:
@@ -64,3 +64,32 @@ def test_transposed_signs_are_complete_before_they_are_kept(monkeypatch, capturi
         assert done == ["moved"] * 4 and first[0] is not second[0]
     else:
         assert done == ["moved"] * 2 + ["complete"] and first is second
+
+
+def test_reconstruction_enters_its_tensors_device(monkeypatch):
+    """The layer's calls launch on the current device and stream."""
+    inside = []
+
+    @contextlib.contextmanager
+    def on(device, stream):
+        inside.append((device, stream))
+        yield
+        inside.pop()
+
+    def within(value):
+        def call(*a, **kw):
+            assert inside == [(torch.device("cpu"), 1234)]
+            return value
+        return call
+
+    class Step:
+        m = n = 32
+        forward_train = within((torch.zeros(3, 32), None))
+        backward = within((None, "grads"))
+        forward = input_grad = within(torch.zeros(3, 50))
+
+    monkeypatch.setattr(output, "_on", on)
+    monkeypatch.setattr(output, "distill_kl", within(("kl", None)))
+    got = output.reconstruction_step(Step(), Step(), torch.zeros(3, 32), torch.zeros(3, 50),
+                                     stream=1234)
+    assert got == ("kl", None, "grads") and not inside
