@@ -168,7 +168,8 @@ AF1_API af1_status af1_token_logprobs(const void *logits, int32_t dtype, int64_t
  *             array otherwise.
  * A token whose two factors are zero, or whose logits are all -infinity, gets
  * zeros whatever its logits hold.  A negative target takes no part in
- * g_logprob; one of V or more gives NaN.
+ * g_logprob; one of V or more gives NaN in the whole row unless its g_logprob is
+ * zero (or NULL), and so does a factor that is NaN.
  */
 AF1_API af1_status af1_token_logprobs_backward(const void *logits, int32_t dtype, int64_t T,
                                                int64_t V, int64_t ld, float scale,

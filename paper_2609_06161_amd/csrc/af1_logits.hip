@@ -552,12 +552,13 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(
   const int64_t y = targets ? targets[r] : -1;
   float gl = g_logprob && y >= 0 ? g_logprob[r] * scale : 0.f;
   const float gh = g_entropy ? g_entropy[r] * scale : 0.f;
-  if ((gl == 0.f && gh == 0.f) || (sv.x == -kInf && sv.y == 0.f)) {
-    const float none[8] = {};
-    for (int64_t i = c0 + threadIdx.x; i < c1; i += kThreads) store8<D>(out, i, V, none);
-    return;
-  }
-  if (y >= V) gl = __builtin_nanf("");
+  const auto fill = [&](float v) {
+    const float all[8] = {v, v, v, v, v, v, v, v};
+    for (int64_t i = c0 + threadIdx.x; i < c1; i += kThreads) store8<D>(out, i, V, all);
+  };
+  if ((gl == 0.f && gh == 0.f) || (sv.x == -kInf && sv.y == 0.f)) return fill(0.f);
+  if (y >= V && gl != 0.f) gl = __builtin_nanf("");
+  if (gl != gl || gh != gh) return fill(__builtin_nanf(""));  // masked entries too
   const float c = scale * kLog2e;
   each_chunk<D>(z + r * ld, c0, c1, V, [&](int first, const auto &x) {
 #pragma unroll
