@@ -187,7 +187,8 @@ AF1_API af1_status af1_token_logprobs_backward(const void *logits, int32_t dtype
  *   student, teacher : device, T rows of V of `dtype`, ld_s and ld_t apart.
  *   weight   : device, fp32[T], or NULL for ones (a mean over tokens is 1/T,
  *              padding 0).
- *   kl       : device, fp32[T], written.
+ *   kl       : device, fp32[T], written; it does not depend on weight, and a
+ *              padding token's may be NaN or infinite (leave it out of a sum).
  *   dstudent : device, T rows of V of dtype, ldd apart, written; NULL for the
  *              loss alone.  It may be the student's own array where ldd = ld_s,
  *              and must not overlap any array otherwise.

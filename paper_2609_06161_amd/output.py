@@ -358,7 +358,9 @@ def reconstruction_step(layer, output, x, teacher, weight=None, scale=1.0, grads
 
     layer: DeviceLayer; output: Fp8Linear with n = layer.m; x: [T, layer.n]
     bfloat16; teacher: [T, V] logits (float32 or bfloat16).  Returns (kl [T],
-    dx or None, (ds_out, ds_mid, ds_in)); the sum of weight * kl is the loss."""
+    dx or None, (ds_out, ds_mid, ds_in)); the sum of weight * kl is the loss.
+    A padding token (weight 0) may have any teacher row, its x has to be finite;
+    a kl of it that is not finite is returned as 0."""
     _need(output.n == layer.m, f"the head reads {output.n} features, the layer gives {layer.m}")
     _need(teacher.dtype in (torch.float32, torch.bfloat16), "teacher must be float32 or bfloat16")
     xb = x.view(torch.int16) if x.dtype == torch.bfloat16 else x
@@ -370,4 +372,6 @@ def reconstruction_step(layer, output, x, teacher, weight=None, scale=1.0, grads
         dh = output.input_grad(dlogits)
         dx, grads = layer.backward(xb, dh.view(torch.int16), saved, grads=grads,
                                    accumulate=accumulate, want_dx=want_dx)
+        if weight is not None:
+            kl = torch.where(weight == 0, kl.nan_to_num(0.0, 0.0), kl)
     return kl, dx, grads
