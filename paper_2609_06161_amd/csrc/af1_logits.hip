@@ -597,7 +597,8 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(
 // statistics, waits for the others' and joins them all in the parts' order.
 // Waiting is bounded: statistics that do not arrive (their block has found no
 // place on the device yet) are computed by the block that misses them, from the
-// logits, with the same operations.  2048 rows of 128256 bf16 with the gradient:
+// logits, with the same operations.  Rows of more parts than the device holds at
+// once get their statistics from a launch of their own.  2048 rows of 128256 bf16 with the gradient:
 // 321 us, 4.9 TB/s (reading both rows again for the second pass: 517); 45 rows of
 // 50257 fp32 15 us.
 // ---------------------------------------------------------------------------
@@ -669,6 +670,25 @@ __device__ __forceinline__ void part_stats(const typename D::raw *s, const typen
   __syncthreads();
   a = block_join<false>(a, c, l.wave);
   b = block_join<false>(b, c, l.wave + kWaves);
+}
+
+// Statistics of every part, for rows whose parts do not all fit the device at
+// once: those that run would wait for the others in vain and compute each of
+// them themselves.
+template <typename D>
+__global__ __launch_bounds__(kThreads) void kl_stats_kernel(const typename D::raw *zs,
+                                                            const typename D::raw *zt, int64_t T,
+                                                            KlArgs g) {
+  __shared__ KlLds l;
+  const int64_t r = blockIdx.x / g.parts.count;
+  const int64_t c0 = blockIdx.x % g.parts.count * g.parts.size;
+  Stat a, b;
+  part_stats<D>(zs + r * g.ld_s, zt + r * g.ld_t, c0, min(c0 + g.parts.size, (g.V + 7) / 8), g.V,
+                g.scale * kLog2e, l, a, b);
+  if (threadIdx.x == 0) {
+    g.stats[blockIdx.x] = pack2(a.m, a.Z);
+    g.stats[T * g.parts.count + blockIdx.x] = pack2(b.m, b.Z);
+  }
 }
 
 // The rows' statistics from all parts'; every thread of the block calls it.
@@ -964,13 +984,18 @@ constexpr int64_t kKlBlocks = 256;
 struct KlPlan {
   bool few;
   Parts parts;
+  // a row's parts are more than half of the workgroups that the device holds at
+  // once (four a compute unit): their statistics take a launch of their own.
+  // From 4.2 million fp32 or 8.4 million 16-bit logits; one row of 2^24 fp32 with
+  // the gradient: 134 us.
+  bool stats_first() const { return parts.count > 2 * device_cus(); }
 };
 
 KlPlan plan_kl(int dtype, int64_t T, int64_t V) {
   return with_type(dtype, [&](auto d) {
     using D = decltype(d);
     const int64_t chunks = (V + 7) / 8;
-    KlPlan p;
+    KlPlan p{};
     for (bool few : {false, true}) {
       const int64_t most = (int64_t)kl_chunks<D>(few) * kThreads, n = (chunks + most - 1) / most;
       // as even as whole turns of the block allow
@@ -1007,7 +1032,15 @@ hipError_t launch_distill_kl(const Rows &z, const void *teacher, int64_t ld_t, f
     g.done = reinterpret_cast<int *>(g.sums + blocks);
     kl_clear_kernel<<<(unsigned)((2 * blocks + kThreads - 1) / kThreads), kThreads, 0, s>>>(
         g.stats, 2 * blocks, g.done, z.T);
-    const hipError_t e = hipGetLastError();
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && plan.stats_first())
+      e = with_type(z.dtype, [&](auto d) {
+        using D = decltype(d);
+        kl_stats_kernel<D><<<(unsigned)blocks, kThreads, 0, s>>>(
+            static_cast<const typename D::raw *>(z.p), static_cast<const typename D::raw *>(teacher),
+            z.T, g);
+        return hipGetLastError();
+      });
     if (e != hipSuccess) return e;
   }
   return with_type(z.dtype, [&](auto d) {
@@ -1024,3 +1057,13 @@ hipError_t launch_distill_kl(const Rows &z, const void *teacher, int64_t ld_t, f
 }
 
 }  // namespace af1h
+
+#ifdef AF1_TEST_BUILD
+// Parts of a KL row, and whether their statistics take a launch of their own.
+extern "C" AF1_API int af1_test_kl_plan(int32_t dtype, int64_t T, int64_t V, int32_t *out) {
+  const af1h::KlPlan p = af1h::plan_kl(dtype, T, V);
+  out[0] = p.parts.count;
+  out[1] = p.stats_first();
+  return 0;
+}
+#endif
