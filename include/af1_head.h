@@ -144,7 +144,7 @@ AF1_API af1_status af1_fp8_linear(const af1_fp8_matrix *W, const void *x, int32_
  * Masked logits (-infinity) have probability 0 and add nothing.  A row whose
  * logits are all -infinity has lse and log probabilities of -infinity and
  * entropy 0.  A row with NaN or +infinity has NaN results (its indices are
- * still ordered).  scale: finite and positive (AF1_ERR_SHAPE).
+ * still ordered).  scale: positive, at most 2.3e38 (AF1_ERR_SHAPE).
  * One pass over the logits; sums in fp32, about the largest logit.
  */
 AF1_API size_t af1_token_logprobs_workspace_bytes(int64_t T, int64_t V, int32_t k);

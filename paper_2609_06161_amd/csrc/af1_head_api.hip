@@ -71,7 +71,8 @@ bool rows_ok(int64_t V, int64_t ld) {
   return V >= 1 && V <= AF1_HEAD_MAX_VOCAB && ld >= V && ld <= ((int64_t)1 << 32);
 }
 bool tokens_ok(int64_t T) { return T >= 0 && T <= AF1_HEAD_MAX_TOKENS; }
-bool scale_ok(float s) { return s > 0.f && s <= 3.402823466e38f; }
+// the kernels multiply by scale log2(e), which has to be finite
+bool scale_ok(float s) { return s > 0.f && s <= 2.3e38f; }
 
 // Whether any two of the spans overlap, the first `outs` of them (written)
 // against all; spans of absent arrays are empty.
