@@ -1186,14 +1186,30 @@ hipError_t launch_strips(const FewArgs &g, hipStream_t s) {
 // 4096 19 and 23); fewer strips are shared by as many waves as fill the device
 // (16384 x 4096: by two 13.9, alone 18.5; 8192 x 28672: by four 42, by eight 48;
 // 4096 x 4096: by eight 5.2, by four 6.9).
+int strip_split(int64_t m, int64_t n) {
+  const int64_t strips = (m + 15) / 16, cus = device_cus();
+  if (strips > 4 * cus && blocks_up(n) <= kStripBlocks) return 1;
+  return strips >= 4 * cus ? 2 : strips >= 2 * cus ? 4 : 8;
+}
+
 template <typename D, int kXFormat, int kWFormat, int kOut>
 hipError_t launch_strip_form(const FewArgs &g, hipStream_t s) {
-  const int64_t strips = (g.m + 15) / 16, cus = device_cus();
-  if (strips > 4 * cus && blocks_up(g.n) <= kStripBlocks)
-    return launch_strips<D, kXFormat, kWFormat, kOut, 1>(g, s);
-  if (strips >= 4 * cus) return launch_strips<D, kXFormat, kWFormat, kOut, 2>(g, s);
-  if (strips >= 2 * cus) return launch_strips<D, kXFormat, kWFormat, kOut, 4>(g, s);
-  return launch_strips<D, kXFormat, kWFormat, kOut, 8>(g, s);
+  switch (strip_split(g.m, g.n)) {
+    case 1: return launch_strips<D, kXFormat, kWFormat, kOut, 1>(g, s);
+    case 2: return launch_strips<D, kXFormat, kWFormat, kOut, 2>(g, s);
+    case 4: return launch_strips<D, kXFormat, kWFormat, kOut, 4>(g, s);
+    default: return launch_strips<D, kXFormat, kWFormat, kOut, 8>(g, s);
+  }
+}
+
+// Whether the strips' workgroups round up to 16 tokens themselves.
+bool strips_round(int64_t n, int64_t T) {
+  return blocks_up(n) <= kStripBlocks && T * blocks_up(n) <= kOwnPieces;
+}
+
+// Pieces a lane when more tokens are rounded.
+int token_pieces(int64_t n, int64_t T) {
+  return blocks_up(n) * (T / 64) >= 8 * device_cus() ? 4 : 1;
 }
 
 }  // namespace
@@ -1232,7 +1248,7 @@ hipError_t launch_fp8_transpose(const af1_fp8_matrix &W, uint8_t *codes, uint8_t
 
 size_t fp8_linear_workspace_bytes(int64_t m, int64_t n, int64_t T) {
   if (T <= kStripTokens)
-    return blocks_up(n) > kStripBlocks || T * blocks_up(n) > kOwnPieces ? blocks_up(n) * 2064 : 0;
+    return strips_round(n, T) ? 0 : blocks_up(n) * 2064;
   int splits = 1;
   for (int y : {AF1_SRC_F32, AF1_SRC_BF16}) {
     const Plan p = plan_linear(m, n, T, y);
@@ -1248,7 +1264,7 @@ hipError_t launch_linear(const af1_fp8_matrix &W, const void *x, int x_dtype, in
   const XTiles xt = x_tiles(ws, n, T);
   FewArgs few{W.codes, W.scales, x, xt, (int)T, m, n, y};
   if (T <= kStripTokens) {
-    const bool own = T * blocks_up(n) <= kOwnPieces && blocks_up(n) <= kStripBlocks;
+    const bool own = strips_round(n, T);
     few.xt.codes = own ? nullptr : static_cast<uint8_t *>(ws);
     return with_type(x_dtype, [&](auto d) {
       using D = decltype(d);
@@ -1265,7 +1281,7 @@ hipError_t launch_linear(const af1_fp8_matrix &W, const void *x, int x_dtype, in
     using D = decltype(d);
     const auto *rows = static_cast<const typename D::raw *>(x);
     const unsigned C = (unsigned)blocks_up(n);
-    if (C * (T / 64) >= 8 * device_cus())
+    if (token_pieces(n, T) == 4)
       quantize_tokens_kernel<D, kXFormat, 4>
           <<<dim3(C, (unsigned)((T + 63) / 64)), 256, 0, s>>>(rows, T, n, xt);
     else
@@ -1312,6 +1328,20 @@ extern "C" AF1_API int af1_test_linear_plan(int64_t m, int64_t n, int64_t T, int
   const af1h::Plan p = af1h::plan_linear(m, n, T, y_dtype);
   out[0] = p.form;
   out[1] = p.splits;
+  return 0;
+}
+
+// Of up to 16 tokens: the waves that share a strip, whether rows are taken in
+// chunks of columns, and whether a launch in front rounds the tokens.  Of more:
+// out[0] pieces a lane when they are rounded.
+extern "C" AF1_API int af1_test_tokens_plan(int64_t m, int64_t n, int64_t T, int32_t *out) {
+  if (T > af1h::kStripTokens) {
+    out[0] = af1h::token_pieces(n, T);
+    return 0;
+  }
+  out[0] = af1h::strip_split(m, n);
+  out[1] = af1h::blocks_up(n) > af1h::kStripBlocks;
+  out[2] = !af1h::strips_round(n, T);
   return 0;
 }
 #endif
