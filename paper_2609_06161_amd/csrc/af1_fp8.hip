@@ -975,14 +975,10 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(FewArgs g) {
     const int k = threadIdx.x & 15;
     for (int piece = threadIdx.x >> 4; piece < g.T * C; piece += 4 * kStripWaves) {
       const int t = piece / C, J = piece % C;
-      float v[8], amax = 0.f;
-      load8<D>(x + t * n + (int64_t)J * kBlk, k, n - (int64_t)J * kBlk, 0.f, v);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) amax = fmaxf(amax, finite_abs(v[i]));
-#pragma unroll
-      for (int off = 8; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 16));
-      const int e = block_exponent<kXFormat>(amax);
-      *reinterpret_cast<uint2 *>(lds + operand_at(J, t, k)) = encode8<kXFormat>(v, pow2(-e));
+      int e;
+      const uint2 codes = round_piece<D, kXFormat>(
+          load_raw_to<D>(x + t * n + (int64_t)J * kBlk, k, n - (int64_t)J * kBlk, 0.f), e);
+      *reinterpret_cast<uint2 *>(lds + operand_at(J, t, k)) = codes;
       if (k == 0) xs[J * 16 + t] = (uint8_t)(e + 127);
     }
     __syncthreads();
@@ -1182,10 +1178,11 @@ hipError_t launch_strips(const FewArgs &g, hipStream_t s) {
 
 // How many waves share a strip.  Each on its own where that leaves more than half
 // of the compute units a workgroup, since a second round of workgroups starts by
-// rounding x again (one token of 28672 x 8192: 37 us, shared by two 64; 24576 x
-// 4096 19 and 23); fewer strips are shared by as many waves as fill the device
-// (16384 x 4096: by two 13.9, alone 18.5; 8192 x 28672: by four 42, by eight 48;
-// 4096 x 4096: by eight 5.2, by four 6.9).
+// rounding x again; fewer strips are shared by as many waves as fill the device.
+// One token, weights from memory, launches of a graph: 28672 x 8192 50 us, shared
+// by two 57; 18944 x 4096 22 and 26; 17408 x 4096, just beyond the limit, 21 and
+// 26; at it, 16384 x 4096 shared by two 18.5, alone 21; 8192 x 8192 by four 19.5,
+// by two 22, by eight 22; 4096 x 4096 by eight 7.3, by four 9.2.
 int strip_split(int64_t m, int64_t n) {
   const int64_t strips = (m + 15) / 16, cus = device_cus();
   if (strips > 4 * cus && blocks_up(n) <= kStripBlocks) return 1;
