@@ -1066,4 +1066,10 @@ extern "C" AF1_API int af1_test_kl_plan(int32_t dtype, int64_t T, int64_t V, int
   out[1] = p.stats_first();
   return 0;
 }
+
+// Parts of a row of log probabilities.
+extern "C" AF1_API int af1_test_logprobs_plan(int64_t T, int64_t V, int32_t *out) {
+  out[0] = af1h::plan_parts(T, V, af1h::kForwardBlocks, af1h::kMaxParts).count;
+  return 0;
+}
 #endif

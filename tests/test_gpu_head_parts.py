@@ -1,16 +1,19 @@
 """Rows that are several workgroups' work: what each part gives has to arrive.
 
-In most tests one part carries most of a sum, so that losing it, or taking
-another part's in its place, changes the result by far more than 1e-5 of it;
-the sums themselves have at most 1000 additions on any path and terms of one
-sign where it matters, so rounding leaves 2000 u = 1.2e-4 of a term at the very
-most and in squares about 1e-6."""
+One part of a row carries most of a sum, so that losing it, or taking another's
+in its place, changes the result by a tenth and more.  Tolerances count the
+roundings on a path of additions: D of them, a thread's terms (eight a chunk),
+the wave's and the block's trees and the parts in order, beside 60 for a term's
+own; a sum of terms of one sign is within D u of itself, u = 2^-24."""
+import ctypes
+
+import numpy as np
 import pytest
 import torch
 
-from paper_2609_06161_amd import head, output as O
+from paper_2609_06161_amd import af1, build_lib, head, output as O
 
-from test_gpu_head import DEV
+from test_gpu_head import DEV, U
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +60,91 @@ def test_kl_of_rows_beyond_what_runs_at_once(T, dtype):
     own = s.clone()
     k2, d2 = O.distill_kl(own, t, dstudent=own)
     assert torch.equal(k2, kl) and torch.equal(d2, d)
+
+
+@pytest.fixture(scope="module")
+def plans():
+    """(parts of a KL row, parts of a row of log probabilities)."""
+    L = ctypes.CDLL(build_lib.HEAD_TEST_LIB)
+    out = (ctypes.c_int32 * 2)()
+
+    def kl(dtype, T, V):
+        code = af1.AF1_SRC_F32 if dtype == torch.float32 else af1.AF1_SRC_BF16
+        assert L.af1_test_kl_plan(code, ctypes.c_int64(T), ctypes.c_int64(V), out) == 0
+        return out[0]
+
+    def logprobs(T, V):
+        assert L.af1_test_logprobs_plan(ctypes.c_int64(T), ctypes.c_int64(V), out) == 0
+        return out[0]
+    return kl, logprobs
+
+
+def piece(V, parts, p):
+    """The logits of part p: parts are whole turns of 256 threads by eight."""
+    chunks = -(-V // 8)
+    size = -(-(-(-chunks // parts)) // 256) * 2048
+    assert -(-V // size) == parts
+    return slice(p * size, min((p + 1) * size, V)), size // 2048
+
+
+@pytest.mark.parametrize("T,V,dtype,parts", [(2, 140001, torch.float32, 69),
+                                             (2, 300001, torch.bfloat16, 74),
+                                             (4, 600007, torch.float32, 74),
+                                             (3, 20011, torch.float32, 10)])
+def test_every_part_of_a_kl_row(plans, T, V, dtype, parts):
+    """The loss is a sum over the parts, the statistics join theirs.  With most
+    of both masses in one part, D (2 + |u|) u sum p |u| and its like stay under
+    1e-4 of the loss (D = 60 + 64 + 16 + 70, |u| < 1, the loss 0.06 and more)."""
+    assert plans[0](dtype, T, V) == parts
+    g = torch.Generator(device=DEV).manual_seed(parts)
+    base, noise = (torch.randn((T, V), generator=g, device=DEV) for _ in range(2))
+    for p in sorted({0, 1, 31, 62, 63, 64, 65, parts - 2, parts - 1} & set(range(parts))):
+        print(f"kl T={T} V={V} {dtype} part {p} of {parts}", flush=True)
+        at, _ = piece(V, parts, p)
+        share = (at.stop - at.start) / V
+        s, t = base.clone(), base + 0.1 * noise
+        # odds 6 and 2 of the part against the rest
+        t[:, at] += np.log(6 * (1 - share) / share)
+        s[:, at] += np.log(2 * (1 - share) / share)
+        s, t = s.to(dtype), t.to(dtype)
+        want, dwant = kl64(s, t)
+        kl, d = O.distill_kl(s, t)
+        assert (want > 0.06).all()
+        close(kl, want, 1e-4)
+        half = {torch.float32: U, torch.bfloat16: 2.0 ** -8}[dtype]
+        q = 2.0 ** -14 * (log_softmax64(s).exp() + log_softmax64(t).exp())
+        assert ((d.double() - dwant).abs() <= half * (dwant.abs() + q) + q).all()
+        assert torch.equal(O.distill_kl(s, t, grad=False)[0], kl)
+
+
+@pytest.mark.parametrize("T,V,dtype,parts", [(1, 128256, torch.float32, 63),
+                                             (3, 131072, torch.bfloat16, 64),
+                                             (20, 128256, torch.float32, 32),
+                                             (400, 50257, torch.float16, 3),
+                                             (2, 5003, torch.float32, 3)])
+def test_every_part_of_a_row_of_log_probabilities(plans, T, V, dtype, parts):
+    """lse and log probabilities within D u (2 + |value|), entropies within
+    D u (4 + 2 ln V): ln Z and sum p |t| are at most ln V."""
+    assert plans[1](T, V) == parts
+    g = torch.Generator(device=DEV).manual_seed(V)
+    base = torch.randn((T, V), generator=g, device=DEV)
+    for p in sorted({0, 1, parts // 2, parts - 2, parts - 1} & set(range(parts))):
+        print(f"logprobs T={T} V={V} {dtype} part {p} of {parts}", flush=True)
+        at, chunks = piece(V, parts, p)
+        D = 60 + 8 * chunks + 16 + parts
+        z = base.clone()
+        z[:, at] += np.log(6 * (V - at.stop + at.start) / (at.stop - at.start))
+        z = z.to(dtype)
+        y = torch.randint(0, V, (T,), generator=g, device=DEV)
+        y[0] = at.stop - 1
+        lp = log_softmax64(z)
+        H = -(lp.exp() * lp).sum(1)
+        lse = torch.logsumexp(z.double(), 1)
+        got = O.token_logprobs(z, y, 9)
+        want = lp.gather(1, y[:, None])[:, 0]
+        assert ((got.logprob - want).abs() <= D * U * (2 + want.abs())).all()
+        assert ((got.lse - lse).abs() <= D * U * (2 + lse.abs())).all()
+        limit = D * U * (4 + 2 * np.log(V))
+        assert limit < 2e-3 and ((got.entropy - H).abs() <= limit).all()
+        top = torch.sort(z, dim=1, descending=True, stable=True)[1][:, :9]
+        assert torch.equal(got.top_index, top)
