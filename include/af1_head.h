@@ -84,7 +84,8 @@ AF1_API af1_status af1_fp8_quantize(const void *src, int32_t src_dtype, int64_t 
 /*
  * af1_fp8_dequantize -- the values that a matrix stands for, rows x cols of
  * dst_dtype, contiguous.  Exact in fp32, and in bfloat16 wherever the value is
- * not below its normal range; binary16 rounds (nearest even).
+ * not below its normal range; binary16 rounds (nearest even).  Codes of entries
+ * that rounded up to 2^128 are infinite.
  */
 AF1_API af1_status af1_fp8_dequantize(const af1_fp8_matrix *W, void *dst, int32_t dst_dtype,
                                       void *stream);
@@ -194,7 +195,7 @@ AF1_API af1_status af1_token_logprobs_backward(const void *logits, int32_t dtype
  *              and must not overlap any array otherwise.
  *   ws       : device, af1_distill_kl_workspace_bytes(T, V) bytes.
  * kl is summed from the differences of the two logits, not of two logarithms,
- * so a small divergence keeps its digits; none is below 0.
+ * so a small divergence errs by some 1e-8, not by 1e-6; none is below 0.
  * Entries whose p_j is 0 in fp32 add nothing.  Where the student masks
  * (-infinity) an entry of the teacher's, kl is infinite.  A token whose teacher
  * masks everything has kl 0; its gradient is zero, and so are those of tokens

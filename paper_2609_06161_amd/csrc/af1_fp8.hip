@@ -152,7 +152,9 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t *codes,
   }
 }
 
-// Rows of 132 bytes in LDS: a column's bytes lie 33 banks apart.
+// Through rows of 132 bytes in LDS.  A lane gathers a word of the result from four
+// of them, and lanes lie four rows apart: the bank conflicts of that stand behind
+// the copy's time (128256 x 4096 194 us, 5.4 TB/s).
 __global__ __launch_bounds__(256) void transpose_tiles_kernel(const uint8_t *codes,
                                                               const uint8_t *scales, int64_t R,
                                                               int64_t C, uint8_t *codesT,
@@ -812,7 +814,7 @@ __device__ __forceinline__ v4f mul_block(v8i w, v8i x, v4f acc, int sw, int sx) 
 // row's four: 16 columns at 16 q and 16 at 64 + 16 q, so that one load covers
 // 64 bytes of a row), and their sums are added in LDS in the waves' order: all
 // of a row's columns at once without a second launch: 24 tokens of 4096 x 4096 in
-// 12.7 us, tiles over ranges of columns 14.6.
+// 10.4 us with its weights from memory; 64 tokens, by tiles, 14.7.
 // ---------------------------------------------------------------------------
 
 struct FewArgs {
@@ -904,8 +906,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewArgs g) {
 // workgroup needs all of x: few pieces it rounds itself (one launch, no
 // workspace), more are rounded by a launch in front (kOwnPieces).  A ring
 // of kRing blocks is in flight a wave, across the ends of strips: memory sees
-// one unbroken stream.  128256 x 4096: 101 us for one token, 108 for twelve (525
-// MB, 5.2 and 4.9 TB/s); 1024 x 4096 5.4 us, which is latency.  When there are
+// one unbroken stream.  128256 x 4096: 101 us for one token, 103 for twelve (525
+// MB, 5.2 and 5.1 TB/s; 107 with outputs in fp32); 1024 x 4096 6.0 us, which is
+// latency.  When there are
 // fewer strips than waves, kSplit waves share a strip, every kSplit-th block
 // each, and add their sums in LDS in order; rows too long for LDS are taken that
 // way too, a chunk of columns at a time.

@@ -587,7 +587,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(
 //   kl = ln2 A + ln(1 + B),   A = sum p u,   B = sum (p 2^-u - p) = sum (q - p).
 // B is 0 but for rounding.  What the fp32 statistics are off by shifts all u
 // alike, by s say; A then changes by s and ln2 A + ln(1 + B) only by its square,
-// so a divergence that is small beside the logarithms keeps its digits.  u is
+// so a divergence that is small beside the logarithms errs by some 1e-8.  u is
 // taken from the difference of the two logits, and q - p = p (2^-u - 1), the
 // gradient's factor, from u.
 //
