@@ -17,7 +17,7 @@
  *   rows is valid and enqueues nothing.
  * Pointers: logits, tokens, log probabilities and what else belongs to tokens
  *   may be slices of larger arrays and need their element's alignment only;
- *   every other array 16 bytes, as in af1.h.
+ *   every other array, the linear's x and y among them, 16 bytes, as in af1.h.
  * Types: dense arrays are fp32, bfloat16 or binary16 (af1_src_dtype, without
  *   AF1_SRC_I8), row-major.
  * Results repeat bit for bit: every sum is taken in a fixed order.

@@ -598,9 +598,9 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(
 // Waiting is bounded: statistics that do not arrive (their block has found no
 // place on the device yet) are computed by the block that misses them, from the
 // logits, with the same operations.  Rows of more parts than the device holds at
-// once get their statistics from a launch of their own.  2048 rows of 128256 bf16 with the gradient:
-// 321 us, 4.9 TB/s (reading both rows again for the second pass: 517); 45 rows of
-// 50257 fp32 15 us.
+// once get their statistics from a launch of their own.  2048 rows of 128256 bf16
+// with the gradient: 321 us, 4.9 TB/s (reading both rows again for the second
+// pass: 517); 45 rows of 50257 fp32 15 us.
 // ---------------------------------------------------------------------------
 
 struct KlArgs {

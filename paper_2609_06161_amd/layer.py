@@ -29,6 +29,8 @@ def on_stream(stream, device=None):
     if stream is None:
         return contextlib.nullcontext()
     if isinstance(stream, int):
+        if stream == torch.cuda.current_stream(device).cuda_stream:
+            return contextlib.nullcontext()
         stream = (torch.cuda.ExternalStream(stream, device) if stream
                   else torch.cuda.default_stream(device))
     return torch.cuda.stream(stream)

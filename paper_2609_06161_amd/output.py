@@ -3,8 +3,9 @@ probabilities of given tokens and the KL divergence to a teacher, as plain
 calls that check their tensors, provide outputs and workspaces where none are
 given, and forward to the C entry points (include/af1_head.h).
 
-Every call runs on the device of its tensors, on `stream` or that device's
-current stream.  bfloat16 tensors may also be given as int16 bit patterns, the
+Every call runs on the device of its tensors, on `stream` (a torch stream or the
+handle of one) or that device's current stream, and what it allocates belongs to
+that stream.  bfloat16 tensors may also be given as int16 bit patterns, the
 form in which DeviceLayer returns its outputs.  Workspaces (`ws`) are optional;
 one that is passed in must not be used by another call at the same time, which
 two captured graphs that share it would do if they were replayed together.

@@ -2,6 +2,7 @@
 replaced): memory of a call that runs on a given stream has to come from that
 stream's pool, or it is handed to other work while the call still uses it."""
 import contextlib
+import types
 
 import pytest
 import torch
@@ -27,6 +28,8 @@ def entered(monkeypatch):
     monkeypatch.setattr(torch.cuda, "stream", stream)
     monkeypatch.setattr(torch.cuda, "ExternalStream", lambda h, device=None: ("external", h, device))
     monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: ("default", device))
+    monkeypatch.setattr(torch.cuda, "current_stream",
+                        lambda device=None: types.SimpleNamespace(cuda_stream=77))
     return seen
 
 
@@ -39,8 +42,9 @@ def test_an_integer_is_a_streams_handle(entered, handle, want):
 
 
 def test_other_streams(entered):
-    with layer.on_stream(None, Device):
-        assert entered == []
+    for current in (None, 77):
+        with layer.on_stream(current, Device):
+            assert entered == []
     with layer.on_stream("a stream"):
         assert entered == ["a stream"]
 
