@@ -148,3 +148,38 @@ def test_every_part_of_a_row_of_log_probabilities(plans, T, V, dtype, parts):
         assert limit < 2e-3 and ((got.entropy - H).abs() <= limit).all()
         top = torch.sort(z, dim=1, descending=True, stable=True)[1][:, :9]
         assert torch.equal(got.top_index, top)
+
+
+def test_kl_of_long_rows_captured_and_on_two_streams():
+    """Statistics in front of the rows: replayed on new logits with eager calls
+    between, and two such calls at once."""
+    T, V = 2, 4_300_003
+    s, t = (torch.empty((T, V), device=DEV) for _ in range(2))
+    g = torch.Generator(device=DEV).manual_seed(3)
+
+    def fresh():
+        s.normal_(generator=g)
+        t.copy_(s).add_(torch.randn((T, V), generator=g, device=DEV), alpha=0.3)
+
+    fresh()
+    O.distill_kl(s, t)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = O.distill_kl(s, t)
+    for _ in range(3):
+        fresh()
+        want = O.distill_kl(s, t)
+        close(want[0], kl64(s, t)[0], 1e-4)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held[0], want[0]) and torch.equal(held[1], want[1])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for side in streams:
+        with torch.cuda.stream(side):
+            got.append(O.distill_kl(s, t))
+    torch.cuda.synchronize()
+    for kl, d in got:
+        assert torch.equal(kl, want[0]) and torch.equal(d, want[1])
